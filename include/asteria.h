@@ -15,6 +15,13 @@
  *   asteria_soap_step      N = Q_L phi(Q_L^T G Q_R) Q_R^T, phi = Adam in the rotated basis
  *                          (paper Eq. 2)
  *
+ * and, in front of it, the operators of a decoder layer whose weight gradients are the G above, apart from its
+ * plain matrix products:
+ *
+ *   asteria_rms_norm, asteria_rms_norm_backward    norm of a residual sum, optionally with 8-bit output
+ *   asteria_dropout                                elements dropped by a counter-based generator, no stored mask
+ *   asteria_attention, asteria_attention_backward  causal attention over packed sequences, grouped heads
+ *
  * Conventions common to every entry point
  *   - All matrix pointers are DEVICE pointers owned by the caller; descriptor arrays
  *     (asteria_block[], asteria_factor[], ...) and option structs are HOST memory and are
@@ -59,7 +66,8 @@ typedef enum asteria_status {
 
 typedef enum asteria_dtype {
     ASTERIA_F32 = 0,
-    ASTERIA_BF16 = 1
+    ASTERIA_BF16 = 1,
+    ASTERIA_E4M3 = 2 /* 8 bits, 4 exponent, 3 mantissa, largest value 448, no infinities (asteria_rms_norm's output only) */
 } asteria_dtype;
 
 /* how asteria_stats_update accumulates a block's products */
@@ -435,6 +443,104 @@ typedef struct asteria_rblock {
 size_t asteria_soap_reproject_workspace_bytes(const asteria_rblock *blocks, int nblocks);
 asteria_status asteria_soap_reproject(const asteria_rblock *blocks, int nblocks,
                                       void *ws, size_t ws_bytes, void *stream);
+
+/* ---- dropout ----------------------------------------------------------------------------------
+ * Y = X k / (1 - p), k = 0 or 1 per element from a counter-based generator, so that a mask is never stored: the gradient of
+ * dropout is the same call on dY with the same random numbers, and asteria_rms_norm and its backward pass make the same k.
+ * The generator is Philox 4x32 with 10 rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3",
+ * 2011): element (r, c) takes 16 bits of the block with key `seed` and counter (c / 8, r, offset low, offset high), word
+ * (c % 8) / 2, low half first, and is kept where these are >= round(65536 p).  So p is rounded to a multiple of 2^-16 (to
+ * which 1 / (1 - p) belongs, too); k depends on the element's place, not on leading dimensions, types or launches.  A program
+ * takes another `offset` for every tensor and step.  Dropped elements are +0 whatever X holds there.
+ *   p, seed, offset   0 <= p, round(65536 p) <= 65535; p = 0: nothing is dropped
+ *   state             NULL, or device pointer to two uint64 (seed, offset) that are read when the kernel runs, instead of the
+ *                     fields: a captured graph that is replayed takes new numbers from there.
+ * X: rows x cols, fp32 or bf16; Y of the same type; Y may be X (with ldy = ldx).
+ * Errors: NULL X, Y or rng, rows or cols <= 0, ld < cols, bad dtype or p -> INVALID_ARG; more than 2^34 elements -> UNSUPPORTED. */
+typedef struct asteria_rng {
+    uint64_t seed, offset;
+    const uint64_t *state;
+    float p;
+} asteria_rng;
+typedef struct asteria_drop {
+    const void *X;
+    void *Y;
+    int32_t rows, cols, ldx, ldy;
+    int32_t dtype; /* asteria_dtype of X and Y */
+} asteria_drop;
+asteria_status asteria_dropout(const asteria_drop *d, const asteria_rng *rng, void *stream);
+
+/* ---- root-mean-square norm of a residual sum -----------------------------------------------------
+ * Per row of cols <= 16384 elements:  h = R + drop(X),  y = h w / sqrt(mean(h^2) + eps),  in fp32; y comes from the unrounded
+ * h.  R NULL: zero; W NULL: ones; rng NULL: no dropout; H (the sum, what the backward pass and the next residual read) NULL: not
+ * written.  H may be R or X, Y may be X (same type and leading dimension).
+ * y_dtype ASTERIA_E4M3: per row (group = 0) or per 128 columns (group = 128, the last group may be shorter)
+ * scale = max(largest |y|, 2^-100) / 448 and Y = y / scale rounded to the nearest 8-bit value (ties to even); Scale: fp32, rows x
+ * ceil(cols / group), contiguous.  A group with an element that is no number, or infinite, holds no number somewhere; others are
+ * not touched by it.
+ * The backward pass takes the sum H as stored: with r = 1 / sqrt(mean(h^2) + eps), n = dY w,
+ *   dR = dH + r (n - h r^2 mean(n h)),   dX = drop(dR),   dW = sum over rows of dY h r,
+ * dH: the gradient that reaches H by the residual path, or NULL.  dX, dR, dW: NULL = not written.  dR may be dH, dX may be dY
+ * (same type and leading dimension).  dW is summed in fp32 in an order that depends on rows and cols alone.  Workspace: the partial
+ * sums of dW (none without dW: ws may then be NULL).
+ * Errors: NULL X or Y (H or dY), rows or cols <= 0, ld < cols, bad dtype, group, eps (>= 0, finite) or rng -> INVALID_ARG; Scale
+ * missing for an 8-bit Y -> INVALID_ARG; cols > 16384 or rows >= 2^22 -> UNSUPPORTED.                                   */
+typedef struct asteria_norm {
+    const void *X, *R, *W;
+    void *H, *Y;
+    float *Scale;
+    int32_t rows, cols, ldx, ldr, ldh, ldy;
+    int32_t x_dtype, h_dtype, y_dtype, w_dtype; /* of X; of R and H; of Y; of W */
+    int32_t group;
+} asteria_norm;
+asteria_status asteria_rms_norm(const asteria_norm *n, float eps, const asteria_rng *rng, void *stream);
+typedef struct asteria_norm_grad {
+    const void *H, *dY, *W, *dH;
+    void *dX, *dR, *dW;
+    int32_t rows, cols, ldh, lddy, lddh, lddx, lddr;
+    int32_t x_dtype, h_dtype, y_dtype, w_dtype; /* of dX; of H, dH and dR; of dY; of W and dW */
+} asteria_norm_grad;
+size_t asteria_rms_norm_backward_workspace_bytes(const asteria_norm_grad *n);
+asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, const asteria_rng *rng,
+                                         void *ws, size_t ws_bytes, void *stream);
+
+/* ---- causal attention over packed sequences -------------------------------------------------------
+ * The rows 0 .. total - 1 of Q, K, V hold sequences one after the other; sequence s is rows cu[s] .. cu[s + 1] - 1.  For every
+ * head j (its keys and values: head j kv_heads / heads of K, V) and every row i of a sequence
+ *   z_il = scale Q_i . K_l  for the rows l <= i of its sequence,   P_i = softmax(z_i),   O_i = sum_l P_il V_l,
+ *   lse_i = log sum_l exp(z_il)   (natural logarithm, fp32, heads x total; NULL: not written).
+ * Sequences of no rows are allowed; rows before the first and behind the last sequence are neither read nor written.  cu: device
+ * int32[nseq + 1], ascending, within 0 .. total (read when the kernel runs; numbers outside are brought inside, but a descending
+ * cu gives unspecified results); NULL: one sequence of `total` rows, nseq = 1.
+ * Element (i, j, d) of Q lies at Q + i ldq + j hq + d, likewise the others: any strides and alignment; of written arrays rows
+ * and heads may not overlap.  dtype fp32 (fp32 matrix cores) or bf16: products and softmax in fp32, P rounded to bf16 as operand
+ * of P V (and dS in the backward pass).  dim 1 .. 128.
+ * A row depends on no element of another sequence; within a sequence K or V that is no number or infinite may also reach the
+ * up to 31 rows before it.
+ * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i, dP = dO V^T, dS = P (dP - D):
+ *   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dK and dV summed over the heads that share them,
+ * without atomics: every run gives the same bits.
+ * Errors: NULL pointers, sizes <= 0, heads no multiple of kv_heads, bad dtype, scale not positive and finite, negative strides,
+ * written arrays that overlap themselves, cu NULL with nseq > 1 -> INVALID_ARG; dim > 128, or (total / 128 + nseq) heads >= 2^24 -> UNSUPPORTED. */
+typedef struct asteria_attn {
+    const void *Q, *K, *V;
+    void *O; /* written by asteria_attention, read by asteria_attention_backward */
+    float *lse;
+    const int32_t *cu;
+    int64_t ldq, ldk, ldv, ldo, hq, hk, hv, ho; /* strides of a row and of a head, in elements */
+    int32_t total, nseq, heads, kv_heads, dim;
+    int32_t dtype;
+    float scale;
+} asteria_attn;
+typedef struct asteria_attn_grad {
+    const void *dO;
+    void *dQ, *dK, *dV;
+    int64_t lddo, lddq, lddk, lddv, hdo, hdq, hdk, hdv;
+} asteria_attn_grad;
+asteria_status asteria_attention(const asteria_attn *a, void *stream);
+size_t asteria_attention_backward_workspace_bytes(const asteria_attn *a);
+asteria_status asteria_attention_backward(const asteria_attn *a, const asteria_attn_grad *g,
+                                          void *ws, size_t ws_bytes, void *stream);
 
 /* ---- measurement aid (not part of the method) -----------------------------------------------
  * Between asteria_profile_enable and asteria_profile_collect every grouped-GEMM launch made by

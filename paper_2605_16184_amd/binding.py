@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_float, c_int, c_int32, c_size_t, c_void_p, POINTER, Structure
+from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p, POINTER, Structure
 from typing import Optional, Sequence
 
 import torch
@@ -14,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libasteria.so")
 
 OK, INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR, EXCEEDS_STATIC_SCRATCH = range(6)
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 ACC_F32, ACC_F64 = 0, 1
 LAYOUT_FULL, LAYOUT_PACKED = 0, 1
 EPS_RELATIVE, EPS_ABSOLUTE = 0, 1
@@ -64,6 +64,36 @@ class _RBlock(Structure):
                 ("M", c_void_p), ("V", c_void_p), ("permL", c_void_p), ("permR", c_void_p),
                 ("m", c_int32), ("n", c_int32), ("ldql_old", c_int32), ("ldql_new", c_int32),
                 ("ldqr_old", c_int32), ("ldqr_new", c_int32), ("ldm", c_int32), ("ldv", c_int32)]
+
+
+class _Rng(Structure):
+    _fields_ = [("seed", c_uint64), ("offset", c_uint64), ("state", c_void_p), ("p", c_float)]
+
+
+class _Drop(Structure):
+    _fields_ = [("X", c_void_p), ("Y", c_void_p), ("rows", c_int32), ("cols", c_int32), ("ldx", c_int32), ("ldy", c_int32),
+                ("dtype", c_int32)]
+
+
+class _Norm(Structure):
+    _fields_ = [("X", c_void_p), ("R", c_void_p), ("W", c_void_p), ("H", c_void_p), ("Y", c_void_p), ("Scale", c_void_p)] + \
+        [(k, c_int32) for k in ("rows", "cols", "ldx", "ldr", "ldh", "ldy", "x_dtype", "h_dtype", "y_dtype", "w_dtype", "group")]
+
+
+class _NormGrad(Structure):
+    _fields_ = [(k, c_void_p) for k in ("H", "dY", "W", "dH", "dX", "dR", "dW")] + \
+        [(k, c_int32) for k in ("rows", "cols", "ldh", "lddy", "lddh", "lddx", "lddr", "x_dtype", "h_dtype", "y_dtype", "w_dtype")]
+
+
+class _Attn(Structure):
+    _fields_ = [(k, c_void_p) for k in ("Q", "K", "V", "O", "lse", "cu")] + \
+        [(k, c_int64) for k in ("ldq", "ldk", "ldv", "ldo", "hq", "hk", "hv", "ho")] + \
+        [(k, c_int32) for k in ("total", "nseq", "heads", "kv_heads", "dim", "dtype")] + [("scale", c_float)]
+
+
+class _AttnGrad(Structure):
+    _fields_ = [(k, c_void_p) for k in ("dO", "dQ", "dK", "dV")] + \
+        [(k, c_int64) for k in ("lddo", "lddq", "lddk", "lddv", "hdo", "hdq", "hdk", "hdv")]
 
 
 class SoapRefreshOpts(Structure):
@@ -162,6 +192,20 @@ def lib():
         for fn in (L.asteria_sym_pack, L.asteria_sym_unpack):
             fn.restype = c_int
             fn.argtypes = [POINTER(_SymPair), c_int, c_void_p]
+        L.asteria_dropout.restype = c_int
+        L.asteria_dropout.argtypes = [POINTER(_Drop), POINTER(_Rng), c_void_p]
+        L.asteria_rms_norm.restype = c_int
+        L.asteria_rms_norm.argtypes = [POINTER(_Norm), c_float, POINTER(_Rng), c_void_p]
+        L.asteria_rms_norm_backward_workspace_bytes.restype = c_size_t
+        L.asteria_rms_norm_backward_workspace_bytes.argtypes = [POINTER(_NormGrad)]
+        L.asteria_rms_norm_backward.restype = c_int
+        L.asteria_rms_norm_backward.argtypes = [POINTER(_NormGrad), c_float, POINTER(_Rng), c_void_p, c_size_t, c_void_p]
+        L.asteria_attention.restype = c_int
+        L.asteria_attention.argtypes = [POINTER(_Attn), c_void_p]
+        L.asteria_attention_backward_workspace_bytes.restype = c_size_t
+        L.asteria_attention_backward_workspace_bytes.argtypes = [POINTER(_Attn)]
+        L.asteria_attention_backward.restype = c_int
+        L.asteria_attention_backward.argtypes = [POINTER(_Attn), POINTER(_AttnGrad), c_void_p, c_size_t, c_void_p]
         L.asteria_profile_i8_flops.restype = c_int
         L.asteria_profile_i8_flops.argtypes = [POINTER(ctypes.c_double)]
         L.asteria_profile_root_work.restype = c_int
@@ -594,3 +638,214 @@ def sym_pack(items, stream=None) -> None:
 def sym_unpack(items, stream=None) -> None:
     """full <- packed (both triangles), for every (full, packed)."""
     _check(lib().asteria_sym_unpack(_sympairs(items), len(items), _stream(stream)), "asteria_sym_unpack")
+
+
+# ---------------------------------------------------------------------------- operators of a decoder layer
+
+class _On:
+    """The device of a call's tensors, which must be one, made current, and the stream the call is enqueued on: ``stream``, or
+    the device's current one.  Workspaces are allocated on that stream, so that their memory is free for others only behind it."""
+
+    def __init__(self, stream, *tensors):
+        dev = tensors[0].device
+        for t in tensors:
+            if t is not None and (t.device != dev or not t.is_cuda):
+                raise ValueError("need GPU tensors on one device")
+        if stream is not None and stream.device != dev:
+            raise ValueError("the stream belongs to another device than the tensors")
+        self.device, self.given = dev, stream
+        self.guard = None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        self.stream = c_void_p((self.given or torch.cuda.current_stream(self.device)).cuda_stream)
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def workspace(self, ws, need: int):
+        if ws is None and not need:
+            return None, 0
+        if ws is None and self.given is not None:
+            with torch.cuda.stream(self.given):
+                ws = _workspace(None, need, self.device)
+        ws = _workspace(ws, need, self.device)
+        if ws.device != self.device:
+            raise ValueError("workspace on another device than the tensors")
+        return c_void_p(ws.data_ptr()), ws.numel()
+
+
+def _rng(p, seed, offset, state):
+    if not p:
+        return None
+    if not 0.0 <= p < 1.0:
+        raise ValueError("p: a probability below 1")
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed, offset: 64-bit numbers")
+    if state is not None and (not state.is_cuda or state.dtype not in (torch.int64, torch.uint64) or state.numel() < 2 or not state.is_contiguous()):
+        raise ValueError("rng: need a contiguous GPU tensor of two 64-bit numbers (seed, offset)")
+    return _Rng(seed, offset, state.data_ptr() if state is not None else None, p)
+
+
+def _as_mat(t, name, shape, dtype=None):
+    """(pointer, leading dimension) of an optional matrix of a given shape."""
+    if t is None:
+        return None, 0
+    ptr, r, c, ld = _mat(t, name, dtype)
+    if (r, c) != shape:
+        raise ValueError(f"{name}: expected {shape}, got {(r, c)}")
+    return ptr, ld
+
+
+def _vec(t, name, n):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous vector of {n} elements")
+    return t.data_ptr()
+
+
+def dropout(X: torch.Tensor, Y: torch.Tensor, p: float, seed: int = 0, offset: int = 0, rng: Optional[torch.Tensor] = None,
+            stream=None) -> None:
+    """Y = X with elements dropped with probability p (a multiple of 2^-16), the others times 1 / (1 - p); Y may be X.  Which ones is
+    a function of (seed, offset) and of the element's row and column alone: the same call on a gradient is the backward pass.
+    ``rng``: GPU tensor of two 64-bit numbers (seed, offset), read when the kernel runs, instead of the arguments."""
+    with _On(stream, X, Y, rng) as on:
+        d = _Drop()
+        d.X, d.rows, d.cols, d.ldx = _mat(X, "X")
+        d.dtype = _dtype_code(X)
+        d.Y, d.ldy = _as_mat(Y, "Y", (d.rows, d.cols), X.dtype)
+        r = _rng(p, seed, offset, rng) or _Rng(0, 0, None, 0.0)
+        _check(lib().asteria_dropout(ctypes.byref(d), ctypes.byref(r), on.stream), "asteria_dropout")
+
+
+def rms_norm(X: torch.Tensor, Y: torch.Tensor, W: Optional[torch.Tensor] = None, R: Optional[torch.Tensor] = None,
+             H: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, group: int = 0, eps: float = 1e-6,
+             p: float = 0.0, seed: int = 0, offset: int = 0, rng: Optional[torch.Tensor] = None, stream=None) -> None:
+    """H = R + dropout(X), Y = H W / sqrt(mean(H^2) + eps) per row.  R, W, H may be None (zero, ones, not written).  Y of dtype
+    float8_e4m3fn: Y = y / scale with fp32 ``scale`` (rows x 1, or rows x ceil(cols / 128) with ``group`` = 128)."""
+    with _On(stream, X, Y, W, R, H, scale, rng) as on:
+        n = _Norm()
+        n.X, n.rows, n.cols, n.ldx = _mat(X, "X")
+        shape = (n.rows, n.cols)
+        n.x_dtype = _dtype_code(X)
+        n.R, n.ldr = _as_mat(R, "R", shape)
+        n.H, n.ldh = _as_mat(H, "H", shape)
+        if R is not None and H is not None and R.dtype != H.dtype:
+            raise TypeError("R and H must be of one dtype")
+        ref = R if R is not None else H
+        n.h_dtype = _dtype_code(ref) if ref is not None else F32
+        n.Y, n.ldy = _as_mat(Y, "Y", shape)
+        n.y_dtype = E4M3 if Y.dtype == torch.float8_e4m3fn else _dtype_code(Y)
+        n.W, n.w_dtype = _vec(W, "W", n.cols), F32 if W is None else _dtype_code(W)
+        n.group = int(group)
+        if scale is not None:
+            groups = -(-n.cols // 128) if group else 1
+            if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != n.rows * groups:
+                raise ValueError(f"scale: need a contiguous fp32 tensor of {n.rows} x {groups} elements")
+            n.Scale = scale.data_ptr()
+        r = _rng(p, seed, offset, rng)
+        _check(lib().asteria_rms_norm(ctypes.byref(n), float(eps), ctypes.byref(r) if r else None, on.stream), "asteria_rms_norm")
+
+
+def _norm_grad(H, dY, W, dH, dX, dR, dW):
+    n = _NormGrad()
+    n.H, n.rows, n.cols, n.ldh = _mat(H, "H")
+    shape = (n.rows, n.cols)
+    n.h_dtype = _dtype_code(H)
+    n.dY, n.lddy = _as_mat(dY, "dY", shape)
+    n.y_dtype = _dtype_code(dY)
+    n.dH, n.lddh = _as_mat(dH, "dH", shape, H.dtype)
+    n.dR, n.lddr = _as_mat(dR, "dR", shape, H.dtype)
+    n.dX, n.lddx = _as_mat(dX, "dX", shape)
+    n.x_dtype = F32 if dX is None else _dtype_code(dX)
+    if W is not None and dW is not None and W.dtype != dW.dtype:
+        raise TypeError("W and dW must be of one dtype")
+    ref = W if W is not None else dW
+    n.W, n.dW, n.w_dtype = _vec(W, "W", n.cols), _vec(dW, "dW", n.cols), F32 if ref is None else _dtype_code(ref)
+    return n
+
+
+def rms_norm_backward_workspace_bytes(H, dY, W=None, dH=None, dX=None, dR=None, dW=None) -> int:
+    return lib().asteria_rms_norm_backward_workspace_bytes(ctypes.byref(_norm_grad(H, dY, W, dH, dX, dR, dW)))
+
+
+def rms_norm_backward(H: torch.Tensor, dY: torch.Tensor, W: Optional[torch.Tensor] = None, dH: Optional[torch.Tensor] = None,
+                      dX: Optional[torch.Tensor] = None, dR: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None,
+                      eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset: int = 0, rng: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of rms_norm at the stored sum H: dR = dH + the norm's gradient of dY, dX = dropout(dR) with the forward pass's
+    random numbers, dW.  dH (in) and each of dX, dR, dW (out) may be None."""
+    with _On(stream, H, dY, W, dH, dX, dR, dW, rng) as on:
+        n = _norm_grad(H, dY, W, dH, dX, dR, dW)
+        r = _rng(p, seed, offset, rng)
+        ptr, size = on.workspace(ws, lib().asteria_rms_norm_backward_workspace_bytes(ctypes.byref(n)))
+        _check(lib().asteria_rms_norm_backward(ctypes.byref(n), float(eps), ctypes.byref(r) if r else None, ptr, size, on.stream),
+               "asteria_rms_norm_backward")
+
+
+def _heads(t, name, dtype=None, shape=None):
+    """(pointer, row stride, head stride) of a rows x heads x dim tensor."""
+    if t.dim() != 3 or t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name}: need a 3-D tensor (rows, heads, dim) with unit stride along dim")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _attn(Q, K, V, O, lse, cu, scale):
+    a = _Attn()
+    if Q.dim() != 3 or K.dim() != 3:
+        raise ValueError("Q, K: need 3-D tensors (rows, heads, dim)")
+    a.total, a.heads, a.dim = Q.shape
+    a.kv_heads = K.shape[1]
+    a.dtype = _dtype_code(Q)
+    a.Q, a.ldq, a.hq = _heads(Q, "Q")
+    a.K, a.ldk, a.hk = _heads(K, "K", Q.dtype, (a.total, a.kv_heads, a.dim))
+    a.V, a.ldv, a.hv = _heads(V, "V", Q.dtype, (a.total, a.kv_heads, a.dim))
+    a.O, a.ldo, a.ho = _heads(O, "O", Q.dtype, (a.total, a.heads, a.dim))
+    if lse is not None:
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (a.heads, a.total) or not lse.is_contiguous():
+            raise ValueError(f"lse: need a contiguous fp32 tensor of {a.heads} x {a.total} elements")
+        a.lse = lse.data_ptr()
+    a.nseq = 1
+    if cu is not None:
+        if cu.dtype != torch.int32 or cu.dim() != 1 or cu.shape[0] < 2 or not cu.is_contiguous():
+            raise ValueError("cu: need a contiguous int32 GPU tensor of the sequences' first rows and the end")
+        a.cu, a.nseq = cu.data_ptr(), cu.shape[0] - 1
+    a.scale = a.dim ** -0.5 if scale is None and a.dim else scale or 0.0
+    return a
+
+
+def attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, lse: Optional[torch.Tensor] = None,
+              cu: Optional[torch.Tensor] = None, scale: Optional[float] = None, stream=None) -> None:
+    """O = softmax(scale Q K^T, causal within every sequence) V.  Q, O: rows x heads x dim; K, V: rows x kv_heads x dim; sequence s is
+    rows cu[s] .. cu[s + 1] - 1 (``cu``: int32 GPU tensor; None: all rows are one sequence); rows of no sequence are left as they
+    are.  ``lse`` (heads x rows, fp32): what the backward pass needs.  ``scale``: default dim^-1/2."""
+    with _On(stream, Q, K, V, O, lse, cu) as on:
+        a = _attn(Q, K, V, O, lse, cu, scale)
+        _check(lib().asteria_attention(ctypes.byref(a), on.stream), "asteria_attention")
+
+
+def attention_backward_workspace_bytes(Q, K, V, O, lse=None, cu=None) -> int:
+    return lib().asteria_attention_backward_workspace_bytes(ctypes.byref(_attn(Q, K, V, O, lse, cu, None)))
+
+
+def attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, lse: torch.Tensor, dO: torch.Tensor,
+                       dQ: torch.Tensor, dK: torch.Tensor, dV: torch.Tensor, cu: Optional[torch.Tensor] = None,
+                       scale: Optional[float] = None, ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dQ, dK, dV of attention from dO and from the O and lse that attention wrote; rows of no sequence are left as they are."""
+    with _On(stream, Q, K, V, O, lse, dO, dQ, dK, dV, cu) as on:
+        a = _attn(Q, K, V, O, lse, cu, scale)
+        g = _AttnGrad()
+        g.dO, g.lddo, g.hdo = _heads(dO, "dO", Q.dtype, tuple(Q.shape))
+        g.dQ, g.lddq, g.hdq = _heads(dQ, "dQ", Q.dtype, tuple(Q.shape))
+        g.dK, g.lddk, g.hdk = _heads(dK, "dK", Q.dtype, tuple(K.shape))
+        g.dV, g.lddv, g.hdv = _heads(dV, "dV", Q.dtype, tuple(V.shape))
+        ptr, size = on.workspace(ws, lib().asteria_attention_backward_workspace_bytes(ctypes.byref(a)))
+        _check(lib().asteria_attention_backward(ctypes.byref(a), ctypes.byref(g), ptr, size, on.stream), "asteria_attention_backward")

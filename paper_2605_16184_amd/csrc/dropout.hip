@@ -1,0 +1,48 @@
+// asteria_dropout: a matrix with elements dropped by a counter-based generator (rows.h).  Bound by memory: one chunk of eight
+// elements and one block of the generator per thread.
+#include "common.h"
+#include "rows.h"
+
+using namespace asteria;
+
+namespace {
+
+template <typename T>
+__global__ __launch_bounds__(256) void dropout_kernel(const T *X, T *Y, int rows, int cols, int ldx, int ldy, int chunks, Dropper d)
+{
+    read_state(d);
+    const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const int r = (int)(t / (unsigned)chunks), c = (int)(t % (unsigned)chunks);
+    if (r >= rows) return;
+    const int n = cols - c * 8;
+    Chunk<T> x;
+    x.load(X + (size_t)r * ldx + (size_t)c * 8, n);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x.get(e);
+    if (d.threshold) drop_chunk(d, (uint32_t)r, (uint32_t)c, v);
+    store8(Y + (size_t)r * ldy + (size_t)c * 8, v, n);
+}
+
+}  // namespace
+
+extern "C" asteria_status asteria_dropout(const asteria_drop *d, const asteria_rng *rng, void *stream_)
+{
+    if (!d || !rng || !d->X || !d->Y || d->rows <= 0 || d->cols <= 0) return ASTERIA_INVALID_ARG;
+    if (d->ldx < d->cols || d->ldy < d->cols || !valid_dtype(d->dtype)) return ASTERIA_INVALID_ARG;
+    if (d->X == d->Y && d->ldx != d->ldy) return ASTERIA_INVALID_ARG;
+    Dropper k;
+    if (!make_dropper(rng, k)) return ASTERIA_INVALID_ARG;
+    hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);
+    const int chunks = d->cols / 8 + (d->cols % 8 != 0);
+    const size_t blocks = ((size_t)d->rows * chunks + 255) / 256;
+    if (blocks > (size_t)MOST_BLOCKS) return ASTERIA_UNSUPPORTED;
+    if (d->dtype == ASTERIA_BF16)
+        hipLaunchKernelGGL(dropout_kernel<bf16_elem>, dim3((unsigned)blocks), dim3(256), 0, stream, (const bf16_elem *)d->X, (bf16_elem *)d->Y,
+                           d->rows, d->cols, d->ldx, d->ldy, chunks, k);
+    else
+        hipLaunchKernelGGL(dropout_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, stream, (const float *)d->X, (float *)d->Y, d->rows,
+                           d->cols, d->ldx, d->ldy, chunks, k);
+    ASTERIA_HIP_TRY(hipGetLastError());
+    return ASTERIA_OK;
+}
