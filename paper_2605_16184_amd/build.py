@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libasteria.so")
 SOURCES = ["api.hip", "stats.hip", "inverse_root.hip", "precondition.hip", "soap.hip", "packed.hip",
-           "norm.hip", "dropout.hip", "attention.hip"]
+           "norm.hip", "dropout.hip", "attention.hip", "attention_dq.hip", "attention_dkv.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,412 @@
+// Causal attention over packed sequences with grouped heads: what the forward kernel and the two kernels of the backward
+// pass share.
+//
+// One pass over the keys with the running maximum and sum of the softmax; no matrix of scores reaches memory.  The products
+// are arranged so that what comes out of one matrix instruction is an operand of the next without leaving its lane: a
+// 32 x 32 result holds, in lane l, column l % 32 and the rows 8 (i / 4) + 4 (l / 32) + i % 4, i = 0 .. 15; as the second
+// operand of the next product lane l holds column l % 32 and eight of 16 places of the contraction, whose order is free as long
+// as the first operand follows it.  So
+//   forward        S^T = K Q^T,  O^T += V^T P^T             a lane holds one query; V^T read from LDS with transposing loads
+//   gradient of Q  S^T = K Q^T,  dP^T = V dO^T,  dQ^T += K^T dS^T
+//   of K and V     S = Q K^T,  dP = dO V^T,  dV^T += dO^T P,  dK^T += Q^T dS     a lane holds one key
+// In bf16 a product takes v_mfma_f32_32x32x16_bf16; in fp32 the same eight values a lane go through eight
+// v_mfma_f32_32x32x2_f32, each of which takes the pair of places that the two halves of the wavefront hold.
+#pragma once
+#include <math.h>
+#include <type_traits>
+
+#include "common.h"
+#include "planes.h"
+#include "rows.h"
+
+namespace asteria {
+
+typedef float acc16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
+constexpr int ATT_THREADS = 256;      // four wavefronts, NA along the tile that the workgroup owns, NB along the rows it passes over
+
+// ---- operands -----------------------------------------------------------------------------------
+// Tiles of rows in LDS.  rows(): eight elements of one row, 8 h .. of the 16 from d on; cols(): of column d + l % 32 the eight rows
+// 4 h + j % 4 + 8 (j / 4) from r on - the order in which a 32 x 32 result holds its rows.
+template <typename T, int DP> struct Op;
+
+// Rows of whole 16-byte pieces without padding: piece c of row r lies at place c ^ (2 (r % 4) + (r / 4) % 2).  Reads of one piece from
+// eight rows side by side and transposing reads of two pieces from four rows both meet every bank once (a padding that
+// suits the first costs the second a conflict: measured 10 % of the backward pass).
+template <int DP> struct Op<bf16_elem, DP> {
+    typedef bf16_elem T;
+    typedef __bf16 frag __attribute__((ext_vector_type(8)));
+    static constexpr int BLOCKS = 2;          // blocks of 32 staged rows a wavefront takes at a time
+    static constexpr int PITCH = DP > 64 ? 128 : 64;
+    __device__ static __forceinline__ int place(int r, int c) { return r * PITCH + ((c ^ (2 * (r & 3) + ((r >> 2) & 1))) << 3); }
+    __device__ static __forceinline__ acc16 mma(frag a, frag b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    __device__ static __forceinline__ frag rows(const T *tile, int r, int d)
+    {
+        const int l = (int)threadIdx.x & 63;
+        return *reinterpret_cast<const frag *>(tile + place(r + (l & 31), (d >> 3) + (l >> 5)));
+    }
+    __device__ static __forceinline__ frag cols(const T *tile, int r, int d)
+    {
+        // a 16-lane group reads four rows of 16 elements and gets, lane by lane, the columns
+        const int l = (int)threadIdx.x & 63, i = l & 15;
+        const T *q = tile + place(r + 4 * (l >> 5) + (i >> 2), (d >> 3) + 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 4 * (i & 1);
+        union { struct { s16x4 lo, hi; } s; frag f; } u;
+        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
+        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(q + 8 * PITCH));
+        return u.f;
+    }
+    __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c) { *reinterpret_cast<u16x8 *>(tile + place(r, d >> 3)) = c.a; }
+    __device__ static __forceinline__ frag pack(const acc16 &v, int from)
+    {
+        frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (__bf16)v[from + j];
+        return f;
+    }
+    __device__ static __forceinline__ float get(const frag &f, int j) { return (float)f[j]; }
+    __device__ static __forceinline__ frag of(const Chunk<T> &c) { return __builtin_bit_cast(frag, c.a); }
+};
+
+// Rows padded by one piece: reads of a piece from eight rows side by side meet every bank once.  The fp32 matrix cores take 16 times
+// as long as the bf16 ones, so nothing else counts here.
+template <int DP> struct Op<float, DP> {
+    typedef float T;
+    typedef float frag __attribute__((ext_vector_type(8)));
+    static constexpr int BLOCKS = 2;
+    static constexpr int PITCH = DP + 4;
+    __device__ static __forceinline__ acc16 mma(frag a, frag b, acc16 c)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+    __device__ static __forceinline__ frag rows(const T *tile, int r, int d)
+    {
+        const int l = (int)threadIdx.x & 63;
+        const T *p = tile + (r + (l & 31)) * PITCH + d + 8 * (l >> 5);
+        const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+        return frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+    __device__ static __forceinline__ frag cols(const T *tile, int r, int d)
+    {
+        const int l = (int)threadIdx.x & 63;
+        frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = tile[(r + 4 * (l >> 5) + (j & 3) + 8 * (j >> 2)) * PITCH + d + (l & 31)];
+        return f;
+    }
+    __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c)
+    {
+        *reinterpret_cast<f32x4 *>(tile + r * PITCH + d) = c.a;
+        *reinterpret_cast<f32x4 *>(tile + r * PITCH + d + 4) = c.b;
+    }
+    __device__ static __forceinline__ frag pack(const acc16 &v, int from)
+    {
+        frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = v[from + j];
+        return f;
+    }
+    __device__ static __forceinline__ float get(const frag &f, int j) { return f[j]; }
+    __device__ static __forceinline__ frag of(const Chunk<T> &c)
+    {
+        frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = c.get(j);
+        return f;
+    }
+};
+
+__device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// values of a lane and of the one 32 places away, joined
+template <bool MAX> __device__ __forceinline__ float join_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return join<MAX>(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// An array of rows x heads x dim.
+struct AttArray {
+    char *p;
+    int64_t ld, hs;
+};
+struct AttArgs {
+    AttArray Q, K, V, O, dO, dQ, dK, dV;
+    float *lse, *delta;
+    float *part;         // sums over a part of the heads that share keys: 2 x splits x total x kv_heads x dim (dK, then dV), or null
+    const int *cu;
+    int total, nseq, heads, group, dim, splits;
+    float scale;
+};
+
+template <typename T> __device__ __forceinline__ T *att_at(const AttArray &a, int row, int head)
+{
+    return reinterpret_cast<T *>(a.p) + (int64_t)row * a.ld + (int64_t)head * a.hs;
+}
+
+// ---- which tile a workgroup takes ----------------------------------------------------------------
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v)
+{
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+// sums over lanes 0 .. l of the wavefront
+__device__ __forceinline__ int scan_lanes(int v)
+{
+    v = dpp_add<0x111, 0xf>(v);     // from 1, 2, 4, 8 lanes before in a row of 16
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);     // last lane of the row before
+    v = dpp_add<0x143, 0xc>(v);     // last lane of the lower half
+    return v;
+}
+
+struct AttTile {
+    int start, len, index;          // first row and length of the sequence, which tile of it
+};
+
+// Tile `item` of all sequences' tiles of QT rows, those with the most tiles before them in their sequence first (their
+// work is longest in a forward pass).  The workgroups beyond the last tile get false.  All lanes of a wavefront take part.
+template <int QT> __device__ __forceinline__ bool find_tile(const AttArgs &a, int item, AttTile &t)
+{
+    if (!a.cu) {
+        t.start = 0; t.len = a.total;
+        t.index = (a.total + QT - 1) / QT - 1 - item;
+        return t.index >= 0;
+    }
+    const int l = (int)threadIdx.x & 63;
+    auto load = [&](int s, int &start, int &len) {
+        start = len = 0;
+        if (s < a.nseq) {
+            const int b = a.cu[s], e = a.cu[s + 1];
+            start = b < 0 ? 0 : b > a.total ? a.total : b;
+            len = (e > a.total ? a.total : e) - start;
+            len = len < 0 ? 0 : len;
+        }
+    };
+    int start, len;
+    if (a.nseq <= 64) {
+        load(l, start, len);
+        const int tiles = (len + QT - 1) / QT;
+        // how many tiles have this index or a larger one
+        auto from = [&](int index) {
+            const int over = tiles - index;
+            return __builtin_amdgcn_readlane(scan_lanes(over > 0 ? over : 0), 63);
+        };
+        if (from(0) <= item) return false;
+        int lo = 0, hi = (a.total + QT - 1) / QT;
+        while (hi - lo > 1) {                       // the largest index of which there are more than `item`
+            const int mid = (lo + hi) >> 1;
+            if (from(mid) > item) lo = mid; else hi = mid;
+        }
+        const int rank = item - from(lo + 1);
+        const uint64_t have = __ballot(tiles > lo);
+        const bool mine = tiles > lo && __builtin_popcountll(have & ((1ull << l) - 1)) == rank;
+        const int s = __builtin_ctzll(__ballot(mine));
+        t.start = __builtin_amdgcn_readlane(start, s);
+        t.len = __builtin_amdgcn_readlane(len, s);
+        t.index = lo;
+        return true;
+    }
+    // many sequences: one after the other (finding the longest first would read cu several times in every workgroup)
+    int before = 0;
+    for (int s0 = 0; s0 < a.nseq; s0 += 64) {
+        load(s0 + l, start, len);
+        const int tiles = (len + QT - 1) / QT, upto = before + scan_lanes(tiles);
+        const uint64_t past = __ballot(upto > item);
+        if (past) {
+            const int s = __builtin_ctzll(past);
+            t.start = __builtin_amdgcn_readlane(start, s);
+            t.len = __builtin_amdgcn_readlane(len, s);
+            t.index = __builtin_amdgcn_readlane(upto, s) - 1 - item;
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// ---- staging ------------------------------------------------------------------------------------
+// BK rows of dim elements, padded with zeros to DP, from memory to LDS.  Rows at any place go through registers.  Whole
+// 16-byte pieces (DIRECT: att_direct) are loaded to LDS without registers, which is what lets the backward kernels keep two
+// wavefronts a SIMD, into one of two stages while the other is read; rows and columns beyond the ends come as zeros from
+// the bounds of the descriptor.
+template <typename T, int DP, int BK, bool DIRECT> struct AttStage;
+
+template <typename T, int DP, int BK> struct AttStage<T, DP, BK, false> {
+    static constexpr int CH = BK * DP / 8 / ATT_THREADS;
+    static_assert(CH * ATT_THREADS * 8 == BK * DP, "whole chunks");
+    Chunk<T> c[CH];
+    // rows row0 .. row0 + rows - 1 of one head
+    __device__ __forceinline__ void load(const AttArray &a, int row0, int head, int rows, int dim)
+    {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = (int)threadIdx.x + ATT_THREADS * i, r = k / (DP / 8), d = k % (DP / 8) * 8;
+            c[i].zero();
+            if (r < rows && d < dim) c[i].load(att_at<const T>(a, row0 + r, head) + d, dim - d);
+        }
+    }
+    __device__ __forceinline__ void store(T *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = (int)threadIdx.x + ATT_THREADS * i, r = k / (DP / 8), d = k % (DP / 8) * 8;
+            Op<T, DP>::put(lds, r, d, c[i]);
+        }
+    }
+};
+
+template <int DP, int BK> struct AttStage<bf16_elem, DP, BK, true> {
+    typedef Op<bf16_elem, DP> M;
+    static constexpr int CPR = M::PITCH / 8, NI = BK * CPR / ATT_THREADS;      // pieces of a row in LDS, load instructions of a wavefront
+    static_assert(NI * ATT_THREADS == BK * CPR, "whole instructions");
+    i32x4 rsrc;
+    uint32_t at[NI], step;
+    // rows row0 + first .. row0 + rows - 1 of one head
+    __device__ __forceinline__ void init(const AttArray &a, int row0, int head, int first, int rows, int dim)
+    {
+        const uint32_t ld = (uint32_t)a.ld * 2u;
+        rsrc = buffer_rsrc(att_at<const bf16_elem>(a, row0, head), rows > 0 ? (uint32_t)(rows - 1) * ld + (uint32_t)dim * 2u : 0u);
+        step = BK * ld;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int p = (int)threadIdx.x + ATT_THREADS * i, r = p / CPR, c = (p % CPR) ^ (2 * (r & 3) + ((r >> 2) & 1));
+            at[i] = c * 8 < dim ? (uint32_t)(first + r) * ld + (uint32_t)c * 16u : 0x80000000u;
+        }
+    }
+    // the next BK rows to `stage`; the rows after them are next
+    __device__ __forceinline__ void issue(const bf16_elem *stage)
+    {
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const bf16_elem *)stage;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            load_to_lds(rsrc, __builtin_amdgcn_readfirstlane(lds + (threadIdx.x & ~63u) * 16u + ATT_THREADS * 16u * i), at[i], 0);
+            if (at[i] < 0x80000000u) at[i] += step;
+        }
+    }
+};
+
+// Whether an array's rows can be loaded to LDS directly: whole aligned 16-byte pieces, offsets within 31 bits even of the
+// tile beyond the last row.
+inline bool att_direct(const AttArray &a, int dtype, int total, int dim)
+{
+    return dtype == ASTERIA_BF16 && dim % 8 == 0 && a.ld >= dim && a.ld % 8 == 0 && a.hs % 8 == 0 &&
+           (reinterpret_cast<uintptr_t>(a.p) & 15) == 0 && ((int64_t)total + 1024) * a.ld < (1 << 30);
+}
+
+// The second operand of a product over dim: lane l holds row `row` of the array, elements 16 c + 8 h + j.
+template <typename T, int DP>
+__device__ __forceinline__ void load_frags(const AttArray &a, int row, int head, bool valid, int dim, typename Op<T, DP>::frag (&f)[DP / 16])
+{
+    const int h = ((int)threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        const int d = 16 * c + 8 * h;
+        Chunk<T> k;
+        k.zero();
+        if (valid && d < dim) k.load(att_at<const T>(a, row, head) + d, dim - d);
+        f[c] = Op<T, DP>::of(k);
+    }
+}
+
+// Elements 32 t + 8 g + 4 h + 0 .. 3 of the row at p (of dim elements), times f.
+__device__ __forceinline__ void store4(bf16_elem *p_, int n, const float (&v)[4])
+{
+    typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    uint16_t *p = reinterpret_cast<uint16_t *>(p_);
+    u16x4_any b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = f32_bf16(v[e]);
+    if (n >= 4) *reinterpret_cast<u16x4_any *>(p) = b;
+    else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (e < n) p[e] = b[e];
+    }
+}
+__device__ __forceinline__ void store4(float *p, int n, const float (&v)[4])
+{
+    if (n >= 4) *reinterpret_cast<f32x4_any *>(p) = f32x4_any{v[0], v[1], v[2], v[3]};
+    else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (e < n) p[e] = v[e];
+    }
+}
+template <typename TO, int DP>
+__device__ __forceinline__ void store_row(TO *p, int dim, const acc16 (&o)[DP / 32], float f)
+{
+    const int h = ((int)threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * t + 8 * g + 4 * h;
+            const float v[4] = {o[t][4 * g] * f, o[t][4 * g + 1] * f, o[t][4 * g + 2] * f, o[t][4 * g + 3] * f};
+            if (d < dim) store4(p + d, dim - d, v);
+        }
+}
+
+// Adds the results of the NB wavefronts that hold the same 32 rows (wavefronts w, w + NA, ..) into the first one's, through
+// NB / 2 x NA x DP x 32 floats of LDS in halves: 4 -> 2 -> 1.
+template <int DP, int NA, int NB>
+__device__ __forceinline__ void add_wavefronts(float *lds, acc16 (&o)[DP / 32])
+{
+    const int l = (int)threadIdx.x & 63, w = (int)threadIdx.x >> 6, wa = w % NA, wb = w / NA;
+#pragma unroll
+    for (int half = NB / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if (wb >= half && wb < 2 * half) {
+            f32x4 *q = reinterpret_cast<f32x4 *>(lds) + ((wb - half) * NA + wa) * DP * 8;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) q[(4 * t + g) * 64 + l] = f32x4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+        }
+        __syncthreads();
+        if (wb < half) {
+            const f32x4 *q = reinterpret_cast<const f32x4 *>(lds) + (wb * NA + wa) * DP * 8;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 v = q[(4 * t + g) * 64 + l];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][4 * g + e] += v[e];
+                }
+        }
+    }
+}
+
+// Most tiles of qt rows that sequences of `total` rows together can have (total / qt whole ones and one more each).
+inline int64_t att_tiles(const AttArgs &a, int qt)
+{
+    if (!a.cu) return ((int64_t)a.total + qt - 1) / qt;
+    return (int64_t)a.total / qt + (a.nseq < a.total ? a.nseq : a.total);
+}
+// A wavefront for every 32 rows, four of which share a tile of the rows they pass over - or where that gives less than two
+// workgroups a CU, four wavefronts for the same 32 rows, each with a quarter of what is passed over.
+inline bool att_few(const AttArgs &a, int heads) { return att_tiles(a, 128) * heads < 512; }
+
+// Kernels for dims padded to 64, 96 or 128.
+template <typename F> asteria_status att_for_type(int dtype, int dim, bool direct, F f)
+{
+    auto width = [&](auto t, auto direct_) {
+        if (dim <= 64) return f(t, std::integral_constant<int, 64>(), direct_);
+        if (dim <= 96) return f(t, std::integral_constant<int, 96>(), direct_);
+        return f(t, std::integral_constant<int, 128>(), direct_);
+    };
+    if (dtype != ASTERIA_BF16) return width(float(), std::false_type());
+    return direct ? width(bf16_elem(), std::true_type()) : width(bf16_elem(), std::false_type());
+}
+
+asteria_status attention_dq(const AttArgs &a, int dtype, hipStream_t stream);
+asteria_status attention_dkv(const AttArgs &a, int dtype, hipStream_t stream);
+int attention_splits(const AttArgs &a);       // of the heads that share keys, in attention_dkv
+
+}  // namespace asteria

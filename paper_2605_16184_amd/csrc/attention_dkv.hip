@@ -1,0 +1,220 @@
+// Gradients of K and V (attention.h): a wavefront holds the keys and values of 32 KB rows in registers and passes over the
+// rows that see them, in all the heads that share them.
+//
+// Where the heads that share keys are many and the tiles are few, several workgroups take a part of these heads each, leave
+// their sums in fp32 in the workspace, and a second kernel adds them up: without atomics, in one order.
+#include "attention.h"
+#include "gemm.h"
+
+using namespace asteria;
+
+namespace {
+
+template <typename T, int DP, int NA, int NB, bool DIRECT> struct DkvShape {
+    static constexpr int BQ = 32 * (NB > 1 ? NB : Op<T, DP>::BLOCKS);
+    static constexpr size_t TILE = (size_t)BQ * Op<T, DP>::PITCH;
+    static constexpr size_t SUMS = (NB / 2) * NA * DP * 32 * sizeof(float), STAGED = (DIRECT ? 2 : 1) * (2 * TILE * sizeof(T) + 2 * BQ * sizeof(float));
+    static constexpr size_t LDS = STAGED > SUMS ? STAGED : SUMS;
+};
+
+template <typename T, int DP, int KB, int NA, int NB, bool DIRECT>
+__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT) ? 2 : 1) void attention_dkv_kernel(AttArgs a)
+{
+    typedef Op<T, DP> M;
+    typedef DkvShape<T, DP, NA, NB, DIRECT> Shape;
+    constexpr int BQ = Shape::BQ, KT = 32 * KB * NA;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int STAGES = DIRECT ? 2 : 1;
+    T *lq = reinterpret_cast<T *>(lds), *lg = lq + Shape::TILE;
+    float *row_lse = reinterpret_cast<float *>(lq + STAGES * 2 * Shape::TILE), *row_delta = row_lse + BQ;
+    AttTile tile;
+    const int kv_heads = a.heads / a.group, units = kv_heads * a.splits;
+    const int unit = (int)blockIdx.x % units, kvh = unit / a.splits, split = unit % a.splits;
+    if (!find_tile<KT>(a, (int)blockIdx.x / units, tile)) return;
+    const int per = a.group / a.splits, head0 = kvh * a.group + split * per;
+    tile.index = (tile.len + KT - 1) / KT - 1 - tile.index;      // the first keys are seen by the most rows
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = (int)threadIdx.x >> 6, wb = w / NA;
+    const int kw = tile.index * KT + w % NA * 32 * KB, ki = kw + (l & 31);
+    typename M::frag kf[KB][DP / 16], vf[KB][DP / 16];
+    acc16 dk[KB][DP / 32], dv[KB][DP / 32];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        load_frags<T, DP>(a.K, tile.start + ki + 32 * kb, kvh, ki + 32 * kb < tile.len, a.dim, kf[kb]);
+        load_frags<T, DP>(a.V, tile.start + ki + 32 * kb, kvh, ki + 32 * kb < tile.len, a.dim, vf[kb]);
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) { dk[kb][t] = 0.0f; dv[kb][t] = 0.0f; }
+    }
+    const float c = a.scale * LOG2E;
+    const int first = tile.index * KT / BQ, nq = (tile.len + BQ - 1) / BQ;
+    AttStage<T, DP, BQ, DIRECT> sq, sg;
+    float lse = 0.0f, delta = 0.0f;
+    auto load = [&](int head, int q0, int stage) {
+        if constexpr (DIRECT) {
+            if (q0 == first * BQ) {
+                sq.init(a.Q, tile.start, head, q0, tile.len, a.dim);
+                sg.init(a.dO, tile.start, head, q0, tile.len, a.dim);
+            }
+            T *to = reinterpret_cast<T *>(lds) + stage * 2 * Shape::TILE;
+            sq.issue(to);
+            sg.issue(to + Shape::TILE);
+        } else {
+            sq.load(a.Q, tile.start + q0, head, tile.len - q0, a.dim);
+            sg.load(a.dO, tile.start + q0, head, tile.len - q0, a.dim);
+        }
+        if (threadIdx.x < BQ) {
+            const bool in = q0 + (int)threadIdx.x < tile.len;
+            const size_t at_row = (size_t)head * a.total + tile.start + q0 + threadIdx.x;
+            lse = in ? a.lse[at_row] * LOG2E : 0.0f;
+            delta = in ? a.delta[at_row] : 0.0f;
+        }
+    };
+    const int steps = (nq - first) * per;
+    int qt = first, head = head0;
+    load(head, qt * BQ, 0);
+    for (int step = 0; step < steps; ++step) {
+        const int q0 = qt * BQ, stage = DIRECT ? step & 1 : 0;
+        lq = reinterpret_cast<T *>(lds) + stage * 2 * Shape::TILE;
+        lg = lq + Shape::TILE;
+        row_lse = reinterpret_cast<float *>(reinterpret_cast<T *>(lds) + STAGES * 2 * Shape::TILE) + stage * 2 * BQ;
+        row_delta = row_lse + BQ;
+        if constexpr (!DIRECT) {
+            __syncthreads();
+            sq.store(lq);
+            sg.store(lg);
+        }
+        if (threadIdx.x < BQ) { row_lse[threadIdx.x] = lse; row_delta[threadIdx.x] = delta; }
+        if constexpr (DIRECT) wait_lds_loads<0>();
+        __syncthreads();
+        if (++qt == nq) { qt = first; ++head; }
+        if (step + 1 < steps) load(head, qt * BQ, ~step & 1);
+#pragma unroll
+        for (int b_ = 0; b_ < BQ / 32 / NB; ++b_) {
+            const int b = b_ * NB + wb;
+            if (q0 + 32 * b + 31 < kw) continue;                 // rows before this wavefront's keys
+            acc16 s[KB], dp[KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) { s[kb] = 0.0f; dp[kb] = 0.0f; }
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                const typename M::frag q = M::rows(lq, 32 * b, 16 * d), g = M::rows(lg, 32 * b, 16 * d);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    s[kb] = M::mma(q, kf[kb][d], s[kb]);
+                    dp[kb] = M::mma(g, vf[kb][d], dp[kb]);
+                }
+            }
+            const bool edge = q0 + 32 * b < kw + 32 * KB - 1;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = 32 * b + acc_row(i, h);
+                const float rl = row_lse[r], rd = row_delta[r];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, -rl));
+                    dp[kb][i] = s[kb][i] * (dp[kb][i] - rd);
+                    if (edge && q0 + r < ki + 32 * kb) { s[kb][i] = 0.0f; dp[kb][i] = 0.0f; }
+                    if (edge && q0 + r == 0) dp[kb][i] = 0.0f;   // as in the gradient of Q
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                typename M::frag p[KB], ds[KB];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) { p[kb] = M::pack(s[kb], 8 * k); ds[kb] = M::pack(dp[kb], 8 * k); }
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) {
+                    const typename M::frag g = M::cols(lg, 32 * b + 16 * k, 32 * t), q = M::cols(lq, 32 * b + 16 * k, 32 * t);
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) {
+                        dv[kb][t] = M::mma(g, p[kb], dv[kb][t]);
+                        dk[kb][t] = M::mma(q, ds[kb], dk[kb][t]);
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (NB > 1) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), dk[kb]);
+            add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), dv[kb]);
+        }
+        if (wb) return;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        if (ki + 32 * kb >= tile.len) continue;
+        const int row = tile.start + ki + 32 * kb;
+        if (a.part) {
+            float *p = a.part + (((size_t)split * a.total + row) * kv_heads + kvh) * a.dim;
+            store_row<float, DP>(p, a.dim, dk[kb], 1.0f);
+            store_row<float, DP>(p + (size_t)a.splits * a.total * kv_heads * a.dim, a.dim, dv[kb], 1.0f);
+        } else {
+            store_row<T, DP>(att_at<T>(a.dK, row, kvh), a.dim, dk[kb], a.scale);
+            store_row<T, DP>(att_at<T>(a.dV, row, kvh), a.dim, dv[kb], 1.0f);
+        }
+    }
+}
+
+// Adds up the splits: a chunk of eight elements of a row and head per thread, dK in the first half of the grid's y, dV in the second.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_sum_kernel(AttArgs a)
+{
+    const int kv_heads = a.heads / a.group, chunks = (a.dim + 7) / 8, per_row = kv_heads * chunks;
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(t / per_row), kvh = (int)(t % per_row) / chunks, d = (int)(t % chunks) * 8;
+    const int begin = a.cu ? max(a.cu[0], 0) : 0, end = a.cu ? min(a.cu[a.nseq], a.total) : a.total;
+    if (row < begin || row >= end) return;
+    const size_t stride = (size_t)a.total * kv_heads * a.dim;
+    const float *p = a.part + blockIdx.y * a.splits * stride + ((size_t)row * kv_heads + kvh) * a.dim + d;
+    float sum[8] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        Chunk<float> c;
+        c.load(p + s * stride, a.dim - d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += c.get(e);
+    }
+    const float f = blockIdx.y == 0 ? a.scale : 1.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] *= f;
+    store8(att_at<T>(blockIdx.y == 0 ? a.dK : a.dV, row, kvh) + d, sum, a.dim - d);
+}
+
+template <typename T, int DP, int KB, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)
+{
+    static bool configured[MAX_DEVICES] = {};
+    constexpr size_t bytes = DkvShape<T, DP, NA, NB, DIRECT>::LDS;
+    auto kernel = attention_dkv_kernel<T, DP, KB, NA, NB, DIRECT>;
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), bytes, configured); e != hipSuccess) return e;
+    const int64_t blocks = att_tiles(a, 32 * KB * NA) * (a.heads / a.group) * a.splits;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(ATT_THREADS), bytes, stream, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
+    const int64_t threads = (int64_t)a.total * (a.heads / a.group) * ((a.dim + 7) / 8);
+    hipLaunchKernelGGL(attention_sum_kernel<T>, dim3((unsigned)((threads + 255) / 256), 2), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// The sums of a part of the heads are written and read once more in fp32, so as few parts as give the card four workgroups a CU.
+int asteria::attention_splits(const AttArgs &a)
+{
+    const int64_t tiles = att_tiles(a, 128) * (a.heads / a.group);
+    int splits = 1;
+    for (int s = 2; s <= a.group && tiles * splits < 1024; ++s)
+        if (a.group % s == 0) splits = s;
+    return splits;
+}
+
+asteria_status asteria::attention_dkv(const AttArgs &a, int dtype, hipStream_t stream)
+{
+    const bool direct = att_direct(a.Q, dtype, a.total, a.dim) && att_direct(a.dO, dtype, a.total, a.dim);
+    return att_for_type(dtype, a.dim, direct, [&](auto t, auto dp, auto direct_) {
+        typedef decltype(t) T;
+        constexpr int DP = dp();
+        constexpr bool DIRECT = decltype(direct_)::value;
+        ASTERIA_HIP_TRY((att_few(a, a.heads / a.group * a.splits) ? launch<T, DP, 1, 1, 4, DIRECT>(a, stream)
+                                                                   : launch<T, DP, 1, 4, 1, DIRECT>(a, stream)));
+        return ASTERIA_OK;
+    });
+}

@@ -1,0 +1,130 @@
+// Gradient of Q (attention.h), and D = rowsum(dO o O), which the gradients of K and V read.
+#include "attention.h"
+#include "gemm.h"
+
+using namespace asteria;
+
+namespace {
+
+template <typename T, int DP, int NA, int NB, bool DIRECT> struct DqShape {
+    static constexpr int BK = 32 * (NB > 1 ? NB : Op<T, DP>::BLOCKS);
+    static constexpr int TILE = BK * Op<T, DP>::PITCH;
+    static constexpr size_t LDS = (DIRECT ? 4 : 2) * (size_t)TILE * sizeof(T);
+    static_assert(LDS >= (NB / 2) * NA * DP * 32 * sizeof(float), "room for the sums");
+};
+
+template <typename T, int DP, int NA, int NB, bool DIRECT>
+__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttArgs a)
+{
+    typedef Op<T, DP> M;
+    constexpr int BK = DqShape<T, DP, NA, NB, DIRECT>::BK;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int TILE = DqShape<T, DP, NA, NB, DIRECT>::TILE;
+    T *lk = reinterpret_cast<T *>(lds), *lv = lk + TILE;
+    AttTile tile;
+    const int head = (int)blockIdx.x % a.heads, kvh = head / a.group;
+    if (!find_tile<32 * NA>(a, (int)blockIdx.x / a.heads, tile)) return;
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = (int)threadIdx.x >> 6, wb = w / NA;
+    const int q0 = tile.index * 32 * NA, qw = q0 + w % NA * 32, qi = qw + (l & 31);
+    const bool valid = qi < tile.len;
+    typename M::frag q[DP / 16], g[DP / 16];
+    float delta = 0.0f;
+    load_frags<T, DP>(a.O, tile.start + qi, head, valid, a.dim, q);
+    load_frags<T, DP>(a.dO, tile.start + qi, head, valid, a.dim, g);
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta += M::get(q[d], j) * M::get(g[d], j);
+    delta = join_halves<false>(delta);
+    const size_t at_row = (size_t)head * a.total + tile.start + qi;
+    if (valid && h == 0 && wb == 0) a.delta[at_row] = delta;
+    const float lse = valid ? a.lse[at_row] * LOG2E : 0.0f;
+    load_frags<T, DP>(a.Q, tile.start + qi, head, valid, a.dim, q);
+    acc16 o[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) o[t] = 0.0f;
+    const float c = a.scale * LOG2E;
+    const int last = min(tile.len, q0 + 32 * NA), nk = (last + BK - 1) / BK;
+    AttStage<T, DP, BK, DIRECT> sk, sv;
+    if constexpr (DIRECT) {
+        sk.init(a.K, tile.start, kvh, 0, last, a.dim);
+        sv.init(a.V, tile.start, kvh, 0, last, a.dim);
+        sk.issue(lk);
+        sv.issue(lv);
+    } else {
+        sk.load(a.K, tile.start, kvh, last, a.dim);
+        sv.load(a.V, tile.start, kvh, last, a.dim);
+    }
+    for (int kt = 0; kt < nk; ++kt) {
+        const int k0 = kt * BK, next = k0 + BK;
+        if constexpr (DIRECT) {
+            lk = reinterpret_cast<T *>(lds) + (kt & 1) * 2 * TILE;
+            lv = lk + TILE;
+            wait_lds_loads<0>();
+            __syncthreads();
+            if (kt + 1 < nk) {
+                T *to = reinterpret_cast<T *>(lds) + (~kt & 1) * 2 * TILE;
+                sk.issue(to);
+                sv.issue(to + TILE);
+            }
+        } else {
+            __syncthreads();
+            sk.store(lk);
+            sv.store(lv);
+            __syncthreads();
+            if (kt + 1 < nk) {
+                sk.load(a.K, tile.start + next, kvh, last - next, a.dim);
+                sv.load(a.V, tile.start + next, kvh, last - next, a.dim);
+            }
+        }
+#pragma unroll
+        for (int b_ = 0; b_ < BK / 32 / NB; ++b_) {
+            const int b = b_ * NB + wb;
+            if (k0 + 32 * b > qw + 31) continue;
+            acc16 s = 0.0f, dp = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                s = M::mma(M::rows(lk, 32 * b, 16 * d), q[d], s);
+                dp = M::mma(M::rows(lv, 32 * b, 16 * d), g[d], dp);
+            }
+            const bool edge = k0 + 32 * b + 31 > qw;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
+                // a row that sees one key has no gradient through the softmax: zero, not the round-off of dP - D
+                if (edge && (k0 + 32 * b + acc_row(i, h) > qi || qi == 0)) s[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const typename M::frag p = M::pack(s, 8 * k);
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(lk, 32 * b + 16 * k, 32 * t), p, o[t]);
+            }
+        }
+    }
+    if constexpr (NB > 1) add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), o);
+    if (valid && wb == 0) store_row<T, DP>(att_at<T>(a.dQ, tile.start + qi, head), a.dim, o, a.scale);
+}
+
+template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)
+{
+    static bool configured[MAX_DEVICES] = {};
+    constexpr size_t bytes = DqShape<T, DP, NA, NB, DIRECT>::LDS;
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(attention_dq_kernel<T, DP, NA, NB, DIRECT>), bytes, configured); e != hipSuccess) return e;
+    hipLaunchKernelGGL((attention_dq_kernel<T, DP, NA, NB, DIRECT>), dim3((unsigned)(att_tiles(a, 32 * NA) * a.heads)), dim3(ATT_THREADS), bytes, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+asteria_status asteria::attention_dq(const AttArgs &a, int dtype, hipStream_t stream)
+{
+    const bool direct = att_direct(a.K, dtype, a.total, a.dim) && att_direct(a.V, dtype, a.total, a.dim);
+    return att_for_type(dtype, a.dim, direct, [&](auto t, auto dp, auto direct_) {
+        typedef decltype(t) T;
+        constexpr int DP = dp();
+        constexpr bool DIRECT = decltype(direct_)::value;
+        ASTERIA_HIP_TRY((att_few(a, a.heads) ? launch<T, DP, 1, 4, DIRECT>(a, stream) : launch<T, DP, 4, 1, DIRECT>(a, stream)));
+        return ASTERIA_OK;
+    });
+}
