@@ -24,7 +24,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     AttTile tile;
     const int head = (int)blockIdx.x % a.heads, kvh = head / a.group;
     if (!find_tile<32 * NA>(a, (int)blockIdx.x / a.heads, tile)) return;
-    const int l = (int)threadIdx.x & 63, h = l >> 5, w = (int)threadIdx.x >> 6, wa = w % NA, wb = w / NA;
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = w % NA, wb = w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
     typename M::frag q[DP / 16];

@@ -25,6 +25,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
     constexpr int BQ = Shape::BQ, KT = 32 * KB * NA;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int STAGES = DIRECT ? 2 : 1;
+    constexpr bool FROM = sizeof(T) == 2;
     T *lq = reinterpret_cast<T *>(lds), *lg = lq + Shape::TILE;
     float *row_lse = reinterpret_cast<float *>(lq + STAGES * 2 * Shape::TILE), *row_delta = row_lse + BQ;
     AttTile tile;
@@ -33,7 +34,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
     if (!find_tile<KT>(a, (int)blockIdx.x / units, tile)) return;
     const int per = a.group / a.splits, head0 = kvh * a.group + split * per;
     tile.index = (tile.len + KT - 1) / KT - 1 - tile.index;      // the first keys are seen by the most rows
-    const int l = (int)threadIdx.x & 63, h = l >> 5, w = (int)threadIdx.x >> 6, wb = w / NA;
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wb = w / NA;
     const int kw = tile.index * KT + w % NA * 32 * KB, ki = kw + (l & 31);
     typename M::frag kf[KB][DP / 16], vf[KB][DP / 16];
     acc16 dk[KB][DP / 32], dv[KB][DP / 32];
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) { dk[kb][t] = 0.0f; dv[kb][t] = 0.0f; }
     }
-    const float c = a.scale * LOG2E;
+    const float c = a.scale * LOG2E, rscale = 1.0f / a.scale;
     const int first = tile.index * KT / BQ, nq = (tile.len + BQ - 1) / BQ;
     AttStage<T, DP, BQ, DIRECT> sq, sg;
     float lse = 0.0f, delta = 0.0f;
@@ -64,8 +65,8 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
         if (threadIdx.x < BQ) {
             const bool in = q0 + (int)threadIdx.x < tile.len;
             const size_t at_row = (size_t)head * a.total + tile.start + q0 + threadIdx.x;
-            lse = in ? a.lse[at_row] * LOG2E : 0.0f;
-            delta = in ? a.delta[at_row] : 0.0f;
+            lse = in ? a.lse[at_row] * -rscale : 0.0f;
+            delta = in ? -a.delta[at_row] : 0.0f;
         }
     };
     const int steps = (nq - first) * per;
@@ -87,13 +88,22 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
         __syncthreads();
         if (++qt == nq) { qt = first; ++head; }
         if (step + 1 < steps) load(head, qt * BQ, ~step & 1);
-#pragma unroll
+#pragma unroll 1
         for (int b_ = 0; b_ < BQ / 32 / NB; ++b_) {
             const int b = b_ * NB + wb;
             if (q0 + 32 * b + 31 < kw) continue;                 // rows before this wavefront's keys
+            // the sums begin at -lse / scale and at -D of their rows: one instruction an element less each.  In bf16, where P is rounded to
+            // 2^-8 anyway: dim additions on top of a large lse cost fp32 results up to three bits (measured at scores around 100)
             acc16 s[KB], dp[KB];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) { s[kb] = 0.0f; dp[kb] = 0.0f; }
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 rl = *reinterpret_cast<const f32x4 *>(row_lse + 32 * b + 8 * g + 4 * h);
+                const f32x4 rd = *reinterpret_cast<const f32x4 *>(row_delta + 32 * b + 8 * g + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) { s[kb][4 * g + e] = FROM ? rl[e] : 0.0f; dp[kb][4 * g + e] = FROM ? rd[e] : 0.0f; }
+            }
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
                 const typename M::frag q = M::rows(lq, 32 * b, 16 * d), g = M::rows(lg, 32 * b, 16 * d);
@@ -103,18 +113,23 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
                     dp[kb] = M::mma(g, vf[kb][d], dp[kb]);
                 }
             }
-            const bool edge = q0 + 32 * b < kw + 32 * KB - 1;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 32 * b + acc_row(i, h);
-                const float rl = row_lse[r], rd = row_delta[r];
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb) {
-                    s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, -rl));
-                    dp[kb][i] = s[kb][i] * (dp[kb][i] - rd);
-                    if (edge && q0 + r < ki + 32 * kb) { s[kb][i] = 0.0f; dp[kb][i] = 0.0f; }
-                    if (edge && q0 + r == 0) dp[kb][i] = 0.0f;   // as in the gradient of Q
+                for (int i = 0; i < 16; ++i) {
+                    const int r = 32 * b + acc_row(i, h);
+                    s[kb][i] = __builtin_amdgcn_exp2f(FROM ? s[kb][i] * c : __builtin_fmaf(s[kb][i], c, row_lse[r] * c));
+                    dp[kb][i] = s[kb][i] * (FROM ? dp[kb][i] : dp[kb][i] + row_delta[r]);
                 }
+            if (q0 + 32 * b < kw + 32 * KB - 1) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = q0 + 32 * b + acc_row(i, h);
+                        if (r < ki + 32 * kb) s[kb][i] = 0.0f;
+                        if (r < ki + 32 * kb || r == 0) dp[kb][i] = 0.0f;    // row 0: as in the gradient of Q
+                    }
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     AttTile tile;
     const int head = (int)blockIdx.x % a.heads, kvh = head / a.group;
     if (!find_tile<32 * NA>(a, (int)blockIdx.x / a.heads, tile)) return;
-    const int l = (int)threadIdx.x & 63, h = l >> 5, w = (int)threadIdx.x >> 6, wb = w / NA;
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wb = w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + w % NA * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
     typename M::frag q[DP / 16], g[DP / 16];
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     if (valid && h == 0 && wb == 0) a.delta[at_row] = delta;
     const float lse = valid ? a.lse[at_row] * LOG2E : 0.0f;
     load_frags<T, DP>(a.Q, tile.start + qi, head, valid, a.dim, q);
-    acc16 o[DP / 32];
+    acc16 from = -delta, o[DP / 32];          // dP - D: its sums begin at -D
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) o[t] = 0.0f;
     const float c = a.scale * LOG2E;
@@ -81,18 +81,18 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
         for (int b_ = 0; b_ < BK / 32 / NB; ++b_) {
             const int b = b_ * NB + wb;
             if (k0 + 32 * b > qw + 31) continue;
-            acc16 s = 0.0f, dp = 0.0f;
+            acc16 s = 0.0f, dp = from;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
                 s = M::mma(M::rows(lk, 32 * b, 16 * d), q[d], s);
                 dp = M::mma(M::rows(lv, 32 * b, 16 * d), g[d], dp);
             }
-            const bool edge = k0 + 32 * b + 31 > qw;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse)) * dp[i];
+            if (k0 + 32 * b + 31 > qw) {
                 // a row that sees one key has no gradient through the softmax: zero, not the round-off of dP - D
-                if (edge && (k0 + 32 * b + acc_row(i, h) > qi || qi == 0)) s[i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) if (k0 + 32 * b + acc_row(i, h) > qi || qi == 0) s[i] = 0.0f;
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
