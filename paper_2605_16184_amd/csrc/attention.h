@@ -35,29 +35,31 @@ constexpr int ATT_THREADS = 256;      // four wavefronts, NA along the tile that
 // 4 h + j % 4 + 8 (j / 4) from r on - the order in which a 32 x 32 result holds its rows.
 template <typename T, int DP> struct Op;
 
-// Rows of whole 16-byte pieces without padding: piece c of row r lies at place c ^ (2 (r % 4) + (r / 4) % 2).  Reads of one piece from
-// eight rows side by side and transposing reads of two pieces from four rows both meet every bank once (a padding that
-// suits the first costs the second a conflict: measured 10 % of the backward pass).
+// Rows of whole 16-byte pieces without padding: piece c of row r lies at place c ^ swz(r).  LDS serves 256 bytes a cycle: reads of
+// one piece from 16 rows side by side, and transposing reads of four pieces side by side from four rows, both meet every
+// bank once.  All four bits of r that count change the place by exclusive or, so that one offset a lane serves all reads.
 template <int DP> struct Op<bf16_elem, DP> {
     typedef bf16_elem T;
     typedef __bf16 frag __attribute__((ext_vector_type(8)));
     static constexpr int BLOCKS = 2;          // blocks of 32 staged rows a wavefront takes at a time
     static constexpr int PITCH = DP > 64 ? 128 : 64;
-    __device__ static __forceinline__ int place(int r, int c) { return r * PITCH + ((c ^ (2 * (r & 3) + ((r >> 2) & 1))) << 3); }
+    __device__ static __forceinline__ int swz(int r) { return (PITCH == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) + ((r >> 2) & 3); }
+    __device__ static __forceinline__ int place(int r, int c) { return r * PITCH + ((c ^ swz(r)) << 3); }
     __device__ static __forceinline__ acc16 mma(frag a, frag b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    // r a multiple of 32, d of 16
     __device__ static __forceinline__ frag rows(const T *tile, int r, int d)
     {
         const int l = (int)threadIdx.x & 63;
-        return *reinterpret_cast<const frag *>(tile + place(r + (l & 31), (d >> 3) + (l >> 5)));
+        return *reinterpret_cast<const frag *>(tile + (place(l & 31, l >> 5) ^ d) + r * PITCH);
     }
+    // r a multiple of 16, d of 32: a 16-lane group reads four rows of 16 elements and gets, lane by lane, the columns
     __device__ static __forceinline__ frag cols(const T *tile, int r, int d)
     {
-        // a 16-lane group reads four rows of 16 elements and gets, lane by lane, the columns
         const int l = (int)threadIdx.x & 63, i = l & 15;
-        const T *q = tile + place(r + 4 * (l >> 5) + (i >> 2), (d >> 3) + 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 4 * (i & 1);
+        const int q = (place(4 * (l >> 5) + (i >> 2), 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 4 * (i & 1)) ^ d;
         union { struct { s16x4 lo, hi; } s; frag f; } u;
-        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
-        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(q + 8 * PITCH));
+        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + q + r * PITCH));
+        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + (q ^ 16) + (r + 8) * PITCH));   // swz(r + 8) = swz(r) ^ 2
         return u.f;
     }
     __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c) { *reinterpret_cast<u16x8 *>(tile + place(r, d >> 3)) = c.a; }
@@ -267,29 +269,31 @@ template <int DP, int BK> struct AttStage<bf16_elem, DP, BK, true> {
     typedef Op<bf16_elem, DP> M;
     static constexpr int CPR = M::PITCH / 8, NI = BK * CPR / ATT_THREADS;      // pieces of a row in LDS, load instructions of a wavefront
     static_assert(NI * ATT_THREADS == BK * CPR, "whole instructions");
-    i32x4 rsrc;
-    uint32_t at[NI], step;
+    uint64_t base;
+    int left, step;        // bytes from there to the end, and to the next tile
+    uint32_t at[NI];
     // rows row0 + first .. row0 + rows - 1 of one head
     __device__ __forceinline__ void init(const AttArray &a, int row0, int head, int first, int rows, int dim)
     {
-        const uint32_t ld = (uint32_t)a.ld * 2u;
-        rsrc = buffer_rsrc(att_at<const bf16_elem>(a, row0, head), rows > 0 ? (uint32_t)(rows - 1) * ld + (uint32_t)dim * 2u : 0u);
+        const int ld = (int)a.ld * 2;
+        base = reinterpret_cast<uint64_t>(att_at<const bf16_elem>(a, row0 + first, head));
+        left = (rows - first - 1) * ld + dim * 2;
         step = BK * ld;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int p = (int)threadIdx.x + ATT_THREADS * i, r = p / CPR, c = (p % CPR) ^ (2 * (r & 3) + ((r >> 2) & 1));
-            at[i] = c * 8 < dim ? (uint32_t)(first + r) * ld + (uint32_t)c * 16u : 0x80000000u;
+            const int p = (int)threadIdx.x + ATT_THREADS * i, r = p / CPR, c = (p % CPR) ^ M::swz(r);
+            at[i] = c * 8 < dim ? (uint32_t)(r * ld + c * 16) : 0x80000000u;
         }
     }
     // the next BK rows to `stage`; the rows after them are next
     __device__ __forceinline__ void issue(const bf16_elem *stage)
     {
-        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const bf16_elem *)stage;
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const bf16_elem *)stage + (threadIdx.x & ~63u) * 16u;
+        const i32x4 rsrc = buffer_rsrc(reinterpret_cast<const void *>(base), (uint32_t)max(left, 0));
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            load_to_lds(rsrc, __builtin_amdgcn_readfirstlane(lds + (threadIdx.x & ~63u) * 16u + ATT_THREADS * 16u * i), at[i], 0);
-            if (at[i] < 0x80000000u) at[i] += step;
-        }
+        for (int i = 0; i < NI; ++i) load_to_lds(rsrc, __builtin_amdgcn_readfirstlane(lds) + ATT_THREADS * 16u * i, at[i], 0);
+        base += (uint32_t)step;
+        left -= step;
     }
 };
 
