@@ -30,6 +30,9 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
 constexpr int ATT_THREADS = 256;      // four wavefronts, NA along the tile that the workgroup owns, NB along the rows it passes over
 
+// The place in LDS of a pointer to it: the low half of its address.
+__device__ __forceinline__ uint32_t lds_place(const void *p) { return (uint32_t)reinterpret_cast<uintptr_t>(p); }
+
 // ---- operands -----------------------------------------------------------------------------------
 // Tiles of rows in LDS.  rows(): eight elements of one row, 8 h .. of the 16 from d on; cols(): of column d + l % 32 the eight rows
 // 4 h + j % 4 + 8 (j / 4) from r on - the order in which a 32 x 32 result holds its rows.
@@ -46,20 +49,29 @@ template <int DP> struct Op<bf16_elem, DP> {
     __device__ static __forceinline__ int swz(int r) { return (PITCH == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) + ((r >> 2) & 3); }
     __device__ static __forceinline__ int place(int r, int c) { return r * PITCH + ((c ^ swz(r)) << 3); }
     __device__ static __forceinline__ acc16 mma(frag a, frag b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    // What a lane reads of a tile (at a multiple of 256 bytes): the exclusive or with d goes last, on the address, so that it takes
+    // one instruction a read and no register over the loop.
+    struct Tile {
+        uint32_t r, c;
+        __device__ __forceinline__ explicit Tile(const T *tile)
+        {
+            const int l = (int)threadIdx.x & 63, i = l & 15;
+            const uint32_t at = lds_place(tile);
+            r = at + 2 * place(l & 31, l >> 5);
+            c = at + 2 * (place(4 * (l >> 5) + (i >> 2), 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 4 * (i & 1));
+        }
+    };
     // r a multiple of 32, d of 16
-    __device__ static __forceinline__ frag rows(const T *tile, int r, int d)
+    __device__ static __forceinline__ frag rows(const Tile &t, int r, int d)
     {
-        const int l = (int)threadIdx.x & 63;
-        return *reinterpret_cast<const frag *>(tile + (place(l & 31, l >> 5) ^ d) + r * PITCH);
+        return *reinterpret_cast<__attribute__((address_space(3))) const frag *>((t.r ^ (2 * d)) + r * PITCH * 2);
     }
     // r a multiple of 16, d of 32: a 16-lane group reads four rows of 16 elements and gets, lane by lane, the columns
-    __device__ static __forceinline__ frag cols(const T *tile, int r, int d)
+    __device__ static __forceinline__ frag cols(const Tile &t, int r, int d)
     {
-        const int l = (int)threadIdx.x & 63, i = l & 15;
-        const int q = (place(4 * (l >> 5) + (i >> 2), 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 4 * (i & 1)) ^ d;
         union { struct { s16x4 lo, hi; } s; frag f; } u;
-        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + q + r * PITCH));
-        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + (q ^ 16) + (r + 8) * PITCH));   // swz(r + 8) = swz(r) ^ 2
+        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((t.c ^ (2 * d)) + r * PITCH * 2));
+        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((t.c ^ (2 * d + 32)) + (r + 8) * PITCH * 2));   // swz(r + 8) = swz(r) ^ 2
         return u.f;
     }
     __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c) { *reinterpret_cast<u16x8 *>(tile + place(r, d >> 3)) = c.a; }
@@ -87,6 +99,7 @@ template <int DP> struct Op<float, DP> {
         for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
         return c;
     }
+    typedef const T *Tile;
     __device__ static __forceinline__ frag rows(const T *tile, int r, int d)
     {
         const int l = (int)threadIdx.x & 63;
@@ -140,7 +153,8 @@ struct AttArray {
 };
 struct AttArgs {
     AttArray Q, K, V, O, dO, dQ, dK, dV;
-    float *lse, *delta;
+    float *lse;
+    float *from;         // gradients: -lse / scale, then -D, heads x total each
     float *part;         // sums over a part of the heads that share keys: 2 x splits x total x kv_heads x dim (dK, then dV), or null
     const int *cu;
     int total, nseq, heads, group, dim, splits;
@@ -269,33 +283,49 @@ template <int DP, int BK> struct AttStage<bf16_elem, DP, BK, true> {
     typedef Op<bf16_elem, DP> M;
     static constexpr int CPR = M::PITCH / 8, NI = BK * CPR / ATT_THREADS;      // pieces of a row in LDS, load instructions of a wavefront
     static_assert(NI * ATT_THREADS == BK * CPR, "whole instructions");
+    static constexpr int RPI = ATT_THREADS / CPR;                              // rows of an instruction of the workgroup: swz(r + RPI) = swz(r)
+    static_assert(RPI % 16 == 0, "one place a lane");
     uint64_t base;
-    int left, step;        // bytes from there to the end, and to the next tile
-    uint32_t at[NI];
+    int left, ld, dim;     // bytes from there to the end, of a row; columns
     // rows row0 + first .. row0 + rows - 1 of one head
-    __device__ __forceinline__ void init(const AttArray &a, int row0, int head, int first, int rows, int dim)
+    __device__ __forceinline__ void init(const AttArray &a, int row0, int head, int first, int rows, int dim_)
     {
-        const int ld = (int)a.ld * 2;
+        ld = (int)a.ld * 2;
         base = reinterpret_cast<uint64_t>(att_at<const bf16_elem>(a, row0 + first, head));
+        dim = dim_;
         left = (rows - first - 1) * ld + dim * 2;
-        step = BK * ld;
+    }
+    // the next BK rows to `stage`; the rows after them are next.  SPARE: a lane's place is made anew for every tile - kept, it is a
+    // register that the gradients of K and V do not have.
+    template <bool SPARE> __device__ __forceinline__ void issue(const bf16_elem *stage)
+    {
+        int t = (int)threadIdx.x;
+        if constexpr (SPARE) asm("" : "+v"(t));
+        const int r = t / CPR, c = (t % CPR) ^ M::swz(r);
+        const uint32_t at = c * 8 < dim ? (uint32_t)(r * ld + c * 16) : 0x80000000u;
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_place(stage) + (threadIdx.x & ~63u) * 16u);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int p = (int)threadIdx.x + ATT_THREADS * i, r = p / CPR, c = (p % CPR) ^ M::swz(r);
-            at[i] = c * 8 < dim ? (uint32_t)(r * ld + c * 16) : 0x80000000u;
+            load_to_lds(buffer_rsrc(reinterpret_cast<const void *>(base), (uint32_t)max(left, 0)), lds + ATT_THREADS * 16u * i, at, 0);
+            base += (uint32_t)(RPI * ld);
+            left -= RPI * ld;
         }
     }
-    // the next BK rows to `stage`; the rows after them are next
-    __device__ __forceinline__ void issue(const bf16_elem *stage)
-    {
-        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const bf16_elem *)stage + (threadIdx.x & ~63u) * 16u;
-        const i32x4 rsrc = buffer_rsrc(reinterpret_cast<const void *>(base), (uint32_t)max(left, 0));
-#pragma unroll
-        for (int i = 0; i < NI; ++i) load_to_lds(rsrc, __builtin_amdgcn_readfirstlane(lds) + ATT_THREADS * 16u * i, at[i], 0);
-        base += (uint32_t)step;
-        left -= step;
-    }
 };
+
+// 64 floats from p on, those from `count` on as zeros, to LDS at `to` (counted by wait_lds_loads).
+__device__ __forceinline__ void load_floats_to_lds(const float *p, int count, const float *to)
+{
+    const i32x4 rsrc = buffer_rsrc(p, (uint32_t)max(count, 0) * 4u);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_place(to));
+    uint32_t t = threadIdx.x;
+    asm("" : "+v"(t));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"((t & 63u) * 4u), "s"(rsrc) : "memory", "m0");
+#pragma clang diagnostic pop
+}
 
 // Whether an array's rows can be loaded to LDS directly: whole aligned 16-byte pieces, offsets within 31 bits even of the
 // tile beyond the last row.
@@ -317,6 +347,19 @@ __device__ __forceinline__ void load_frags(const AttArray &a, int row, int head,
         k.zero();
         if (valid && d < dim) k.load(att_at<const T>(a, row, head) + d, dim - d);
         f[c] = Op<T, DP>::of(k);
+    }
+}
+
+// The loads of f have arrived behind this: left to their first use, which lies in the loop over the tiles, the wait for them would
+// hold up every step until the next tile's loads have arrived, too.
+template <typename F, int N> __device__ __forceinline__ void arrived(F (&f)[N])
+{
+    typedef int words __attribute__((ext_vector_type(sizeof(F) / 4)));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        words v = __builtin_bit_cast(words, f[i]);
+        asm volatile("" : "+v"(v));
+        f[i] = __builtin_bit_cast(F, v);
     }
 }
 

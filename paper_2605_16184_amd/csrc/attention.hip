@@ -18,13 +18,13 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
 {
     typedef Op<T, DP> M;
     constexpr int BK = FwdShape<T, DP, NA, NB, DIRECT>::BK, NBLK = BK / 32 / NB;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(256))) char lds[];
     constexpr int TILE = FwdShape<T, DP, NA, NB, DIRECT>::TILE;
     T *lk = reinterpret_cast<T *>(lds), *lv = lk + TILE;
     AttTile tile;
     const int head = (int)blockIdx.x % a.heads, kvh = head / a.group;
     if (!find_tile<32 * NA>(a, (int)blockIdx.x / a.heads, tile)) return;
-    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = w % NA, wb = w / NA;
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
     typename M::frag q[DP / 16];
@@ -41,12 +41,13 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     if constexpr (DIRECT) {
         sk.init(a.K, tile.start, kvh, 0, last, a.dim);
         sv.init(a.V, tile.start, kvh, 0, last, a.dim);
-        sk.issue(lk);
-        sv.issue(lv);
+        sk.template issue<false>(lk);
+        sv.template issue<false>(lv);
     } else {
         sk.load(a.K, tile.start, kvh, last, a.dim);
         sv.load(a.V, tile.start, kvh, last, a.dim);
     }
+    arrived(q);
     for (int kt = 0; kt < nk; ++kt) {
         const int k0 = kt * BK + wb * 32 * NBLK, next = (kt + 1) * BK;   // k0: of this wavefront's keys
         if constexpr (DIRECT) {
@@ -56,8 +57,8 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
             __syncthreads();
             if (kt + 1 < nk) {
                 T *to = reinterpret_cast<T *>(lds) + (~kt & 1) * 2 * TILE;
-                sk.issue(to);
-                sv.issue(to + TILE);
+                sk.template issue<false>(to);
+                sv.template issue<false>(to + TILE);
             }
         } else {
             __syncthreads();
@@ -69,6 +70,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
                 sv.load(a.V, tile.start + next, kvh, last - next, a.dim);
             }
         }
+        const typename M::Tile tk(lk + 32 * wb * NBLK * M::PITCH), tv(lv + 32 * wb * NBLK * M::PITCH);
         if (k0 > qw + 31) continue;                              // behind its rows
         acc16 s[NBLK];
 #pragma unroll
@@ -76,7 +78,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-            for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(lk, 32 * (wb * NBLK + b), 16 * d), q[d], s[b]);
+            for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s[b]);
         if (k0 + 32 * NBLK - 1 > qw) {
 #pragma unroll
             for (int b = 0; b < NBLK; ++b)
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
             for (int k = 0; k < 2; ++k) {
                 const typename M::frag p = M::pack(s[b], 8 * k);
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(lv, 32 * (wb * NBLK + b) + 16 * k, 32 * t), p, o[t]);
+                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tv, 32 * b + 16 * k, 32 * t), p, o[t]);
             }
         }
     }
@@ -212,7 +214,7 @@ extern "C" size_t asteria_attention_backward_workspace_bytes(const asteria_attn 
 {
     if (validate(a, false) != ASTERIA_OK) return 0;
     const AttArgs k = args_of(a);
-    return Carver::need((size_t)a->total * a->heads, sizeof(float)) + Carver::need(part_elems(k, attention_splits(k)), sizeof(float));
+    return Carver::need(2 * (size_t)a->total * a->heads, sizeof(float)) + Carver::need(part_elems(k, attention_splits(k)), sizeof(float));
 }
 
 extern "C" asteria_status asteria_attention_backward(const asteria_attn *a, const asteria_attn_grad *g,
@@ -232,7 +234,7 @@ extern "C" asteria_status asteria_attention_backward(const asteria_attn *a, cons
     k.dK = array(g->dK, g->lddk, g->hdk);
     k.dV = array(g->dV, g->lddv, g->hdv);
     Carver cv(ws);
-    k.delta = cv.take<float>((size_t)a->total * a->heads);
+    k.from = cv.take<float>(2 * (size_t)a->total * a->heads);
     k.splits = attention_splits(k);
     k.part = k.splits > 1 ? cv.take<float>(part_elems(k, k.splits)) : nullptr;
     ASTERIA_TRY(attention_dq(k, a->dtype, stream));

@@ -11,9 +11,13 @@ using namespace asteria;
 namespace {
 
 template <typename T, int DP, int NA, int NB, bool DIRECT> struct DkvShape {
-    static constexpr int BQ = 32 * (NB > 1 ? NB : Op<T, DP>::BLOCKS);
+    static constexpr bool WIDE = sizeof(T) == 2 && DP == 128 && DIRECT && NB == 1;
+    static constexpr int BQ = 32 * (NB > 1 ? NB : WIDE ? 1 : Op<T, DP>::BLOCKS), ROWS = BQ < 64 ? 64 : BQ;
     static constexpr size_t TILE = (size_t)BQ * Op<T, DP>::PITCH;
-    static constexpr size_t SUMS = (NB / 2) * NA * DP * 32 * sizeof(float), STAGED = (DIRECT ? 2 : 1) * (2 * TILE * sizeof(T) + 2 * BQ * sizeof(float));
+    // Pieces of V that stay in LDS: with heads of 128 a wavefront's registers do not hold all, and what the compiler spilled
+    // would wait behind the loads of the next tile.
+    static constexpr int HELD = WIDE ? 3 : 0;
+    static constexpr size_t SUMS = (NB / 2) * NA * DP * 32 * sizeof(float), STAGED = (DIRECT ? 2 : 1) * (2 * TILE * sizeof(T) + 2 * ROWS * sizeof(float)) + HELD * NA * 64 * 16;
     static constexpr size_t LDS = STAGED > SUMS ? STAGED : SUMS;
 };
 
@@ -23,19 +27,19 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
     typedef Op<T, DP> M;
     typedef DkvShape<T, DP, NA, NB, DIRECT> Shape;
     constexpr int BQ = Shape::BQ, KT = 32 * KB * NA;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(256))) char lds[];
     constexpr int STAGES = DIRECT ? 2 : 1;
     constexpr bool FROM = sizeof(T) == 2;
     T *lq = reinterpret_cast<T *>(lds), *lg = lq + Shape::TILE;
-    float *row_lse = reinterpret_cast<float *>(lq + STAGES * 2 * Shape::TILE), *row_delta = row_lse + BQ;
+    auto rows_of = [&](int stage) { return reinterpret_cast<float *>(reinterpret_cast<T *>(lds) + STAGES * 2 * Shape::TILE) + stage * 2 * Shape::ROWS; };
     AttTile tile;
     const int kv_heads = a.heads / a.group, units = kv_heads * a.splits;
     const int unit = (int)blockIdx.x % units, kvh = unit / a.splits, split = unit % a.splits;
     if (!find_tile<KT>(a, (int)blockIdx.x / units, tile)) return;
     const int per = a.group / a.splits, head0 = kvh * a.group + split * per;
     tile.index = (tile.len + KT - 1) / KT - 1 - tile.index;      // the first keys are seen by the most rows
-    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wb = w / NA;
-    const int kw = tile.index * KT + w % NA * 32 * KB, ki = kw + (l & 31);
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
+    const int kw = tile.index * KT + wa * 32 * KB, ki = kw + (l & 31);
     typename M::frag kf[KB][DP / 16], vf[KB][DP / 16];
     acc16 dk[KB][DP / 32], dv[KB][DP / 32];
 #pragma unroll
@@ -45,7 +49,13 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) { dk[kb][t] = 0.0f; dv[kb][t] = 0.0f; }
     }
-    const float c = a.scale * LOG2E, rscale = 1.0f / a.scale;
+    typedef typename M::frag frag;
+    constexpr int HELD = Shape::HELD, REGS = DP / 16 - HELD;
+    static_assert(HELD == 0 || KB == 1, "one block of keys");
+    frag *held = reinterpret_cast<frag *>(rows_of(STAGES)) + w * HELD * 64 + l;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[64 * i] = vf[0][REGS + i];
+    const float c = a.scale * LOG2E;
     const int first = tile.index * KT / BQ, nq = (tile.len + BQ - 1) / BQ;
     AttStage<T, DP, BQ, DIRECT> sq, sg;
     float lse = 0.0f, delta = 0.0f;
@@ -56,42 +66,51 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
                 sg.init(a.dO, tile.start, head, q0, tile.len, a.dim);
             }
             T *to = reinterpret_cast<T *>(lds) + stage * 2 * Shape::TILE;
-            sq.issue(to);
-            sg.issue(to + Shape::TILE);
+            sq.template issue<true>(to);
+            sg.template issue<true>(to + Shape::TILE);
+            // wavefronts 0 and 2 the rows' -lse / scale, 1 and 3 their -D
+            const int r = (w >> 1) * 64;
+            if (r < BQ) load_floats_to_lds(a.from + ((size_t)(w & 1) * a.heads + head) * a.total + tile.start + q0 + r, tile.len - q0 - r,
+                                           rows_of(stage) + (w & 1) * Shape::ROWS + r);
         } else {
             sq.load(a.Q, tile.start + q0, head, tile.len - q0, a.dim);
             sg.load(a.dO, tile.start + q0, head, tile.len - q0, a.dim);
-        }
-        if (threadIdx.x < BQ) {
-            const bool in = q0 + (int)threadIdx.x < tile.len;
-            const size_t at_row = (size_t)head * a.total + tile.start + q0 + threadIdx.x;
-            lse = in ? a.lse[at_row] * -rscale : 0.0f;
-            delta = in ? -a.delta[at_row] : 0.0f;
+            if (threadIdx.x < BQ) {
+                const bool in = q0 + (int)threadIdx.x < tile.len;
+                const float *p = a.from + (size_t)head * a.total + tile.start + q0 + threadIdx.x;
+                lse = in ? p[0] : 0.0f;
+                delta = in ? p[(size_t)a.heads * a.total] : 0.0f;
+            }
         }
     };
     const int steps = (nq - first) * per;
     int qt = first, head = head0;
     load(head, qt * BQ, 0);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) { arrived(kf[kb]); arrived(vf[kb]); }
     for (int step = 0; step < steps; ++step) {
         const int q0 = qt * BQ, stage = DIRECT ? step & 1 : 0;
         lq = reinterpret_cast<T *>(lds) + stage * 2 * Shape::TILE;
         lg = lq + Shape::TILE;
-        row_lse = reinterpret_cast<float *>(reinterpret_cast<T *>(lds) + STAGES * 2 * Shape::TILE) + stage * 2 * BQ;
-        row_delta = row_lse + BQ;
+        const float *row_lse = rows_of(stage), *row_delta = row_lse + Shape::ROWS;
         if constexpr (!DIRECT) {
             __syncthreads();
             sq.store(lq);
             sg.store(lg);
+            if (threadIdx.x < BQ) { rows_of(0)[threadIdx.x] = lse; rows_of(0)[Shape::ROWS + threadIdx.x] = delta; }
+        } else {
+            wait_lds_loads<0>();
         }
-        if (threadIdx.x < BQ) { row_lse[threadIdx.x] = lse; row_delta[threadIdx.x] = delta; }
-        if constexpr (DIRECT) wait_lds_loads<0>();
         __syncthreads();
         if (++qt == nq) { qt = first; ++head; }
         if (step + 1 < steps) load(head, qt * BQ, ~step & 1);
-#pragma unroll 1
+        const typename M::Tile tq(lq + 32 * wb * M::PITCH), tg(lg + 32 * wb * M::PITCH);
+        row_lse += 32 * wb;
+        row_delta += 32 * wb;
+#pragma unroll
         for (int b_ = 0; b_ < BQ / 32 / NB; ++b_) {
-            const int b = b_ * NB + wb;
-            if (q0 + 32 * b + 31 < kw) continue;                 // rows before this wavefront's keys
+            const int b = b_ * NB, qb = q0 + 32 * (b + wb);
+            if (qb + 31 < kw) continue;                 // rows before this wavefront's keys
             // the sums begin at -lse / scale and at -D of their rows: one instruction an element less each.  In bf16, where P is rounded to
             // 2^-8 anyway: dim additions on top of a large lse cost fp32 results up to three bits (measured at scores around 100)
             acc16 s[KB], dp[KB];
@@ -106,11 +125,11 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
             }
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
-                const typename M::frag q = M::rows(lq, 32 * b, 16 * d), g = M::rows(lg, 32 * b, 16 * d);
+                const typename M::frag q = M::rows(tq, 32 * b, 16 * d), g = M::rows(tg, 32 * b, 16 * d);
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
                     s[kb] = M::mma(q, kf[kb][d], s[kb]);
-                    dp[kb] = M::mma(g, vf[kb][d], dp[kb]);
+                    dp[kb] = M::mma(g, d < REGS ? vf[kb][d] : held[64 * (d - REGS)], dp[kb]);
                 }
             }
 #pragma unroll
@@ -121,12 +140,12 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
                     s[kb][i] = __builtin_amdgcn_exp2f(FROM ? s[kb][i] * c : __builtin_fmaf(s[kb][i], c, row_lse[r] * c));
                     dp[kb][i] = s[kb][i] * (FROM ? dp[kb][i] : dp[kb][i] + row_delta[r]);
                 }
-            if (q0 + 32 * b < kw + 32 * KB - 1) {
+            if (qb < kw + 32 * KB - 1) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int r = q0 + 32 * b + acc_row(i, h);
+                        const int r = qb + acc_row(i, h);
                         if (r < ki + 32 * kb) s[kb][i] = 0.0f;
                         if (r < ki + 32 * kb || r == 0) dp[kb][i] = 0.0f;    // row 0: as in the gradient of Q
                     }
@@ -138,7 +157,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
                 for (int kb = 0; kb < KB; ++kb) { p[kb] = M::pack(s[kb], 8 * k); ds[kb] = M::pack(dp[kb], 8 * k); }
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) {
-                    const typename M::frag g = M::cols(lg, 32 * b + 16 * k, 32 * t), q = M::cols(lq, 32 * b + 16 * k, 32 * t);
+                    const typename M::frag g = M::cols(tg, 32 * b + 16 * k, 32 * t), q = M::cols(tq, 32 * b + 16 * k, 32 * t);
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) {
                         dv[kb][t] = M::mma(g, p[kb], dv[kb][t]);

@@ -1,4 +1,4 @@
-// Gradient of Q (attention.h), and D = rowsum(dO o O), which the gradients of K and V read.
+// Gradient of Q (attention.h); and for the gradients of K and V, at which their sums begin: -lse / scale and -D, D = rowsum(dO o O).
 #include "attention.h"
 #include "gemm.h"
 
@@ -18,14 +18,14 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
 {
     typedef Op<T, DP> M;
     constexpr int BK = DqShape<T, DP, NA, NB, DIRECT>::BK;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(256))) char lds[];
     constexpr int TILE = DqShape<T, DP, NA, NB, DIRECT>::TILE;
     T *lk = reinterpret_cast<T *>(lds), *lv = lk + TILE;
     AttTile tile;
     const int head = (int)blockIdx.x % a.heads, kvh = head / a.group;
     if (!find_tile<32 * NA>(a, (int)blockIdx.x / a.heads, tile)) return;
-    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wb = w / NA;
-    const int q0 = tile.index * 32 * NA, qw = q0 + w % NA * 32, qi = qw + (l & 31);
+    const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
+    const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
     typename M::frag q[DP / 16], g[DP / 16];
     float delta = 0.0f;
@@ -37,8 +37,11 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
         for (int j = 0; j < 8; ++j) delta += M::get(q[d], j) * M::get(g[d], j);
     delta = join_halves<false>(delta);
     const size_t at_row = (size_t)head * a.total + tile.start + qi;
-    if (valid && h == 0 && wb == 0) a.delta[at_row] = delta;
-    const float lse = valid ? a.lse[at_row] * LOG2E : 0.0f;
+    const float lse_ = valid ? a.lse[at_row] : 0.0f, lse = lse_ * LOG2E;
+    if (valid && h == 0 && wb == 0) {
+        a.from[at_row] = -lse_ / a.scale;
+        a.from[(size_t)a.heads * a.total + at_row] = -delta;
+    }
     load_frags<T, DP>(a.Q, tile.start + qi, head, valid, a.dim, q);
     acc16 from = -delta, o[DP / 32];          // dP - D: its sums begin at -D
 #pragma unroll
@@ -49,12 +52,13 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     if constexpr (DIRECT) {
         sk.init(a.K, tile.start, kvh, 0, last, a.dim);
         sv.init(a.V, tile.start, kvh, 0, last, a.dim);
-        sk.issue(lk);
-        sv.issue(lv);
+        sk.template issue<false>(lk);
+        sv.template issue<false>(lv);
     } else {
         sk.load(a.K, tile.start, kvh, last, a.dim);
         sv.load(a.V, tile.start, kvh, last, a.dim);
     }
+    arrived(q);
     for (int kt = 0; kt < nk; ++kt) {
         const int k0 = kt * BK, next = k0 + BK;
         if constexpr (DIRECT) {
@@ -64,8 +68,8 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
             __syncthreads();
             if (kt + 1 < nk) {
                 T *to = reinterpret_cast<T *>(lds) + (~kt & 1) * 2 * TILE;
-                sk.issue(to);
-                sv.issue(to + TILE);
+                sk.template issue<false>(to);
+                sv.template issue<false>(to + TILE);
             }
         } else {
             __syncthreads();
@@ -77,28 +81,29 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
                 sv.load(a.V, tile.start + next, kvh, last - next, a.dim);
             }
         }
+        const typename M::Tile tk(lk + 32 * wb * M::PITCH), tv(lv + 32 * wb * M::PITCH);
 #pragma unroll
         for (int b_ = 0; b_ < BK / 32 / NB; ++b_) {
-            const int b = b_ * NB + wb;
-            if (k0 + 32 * b > qw + 31) continue;
+            const int b = b_ * NB, kb = k0 + 32 * (b + wb);
+            if (kb > qw + 31) continue;
             acc16 s = 0.0f, dp = from;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
-                s = M::mma(M::rows(lk, 32 * b, 16 * d), q[d], s);
-                dp = M::mma(M::rows(lv, 32 * b, 16 * d), g[d], dp);
+                s = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s);
+                dp = M::mma(M::rows(tv, 32 * b, 16 * d), g[d], dp);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse)) * dp[i];
-            if (k0 + 32 * b + 31 > qw) {
+            if (kb + 31 > qw) {
                 // a row that sees one key has no gradient through the softmax: zero, not the round-off of dP - D
 #pragma unroll
-                for (int i = 0; i < 16; ++i) if (k0 + 32 * b + acc_row(i, h) > qi || qi == 0) s[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) if (kb + acc_row(i, h) > qi || qi == 0) s[i] = 0.0f;
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const typename M::frag p = M::pack(s, 8 * k);
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(lk, 32 * b + 16 * k, 32 * t), p, o[t]);
+                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tk, 32 * b + 16 * k, 32 * t), p, o[t]);
             }
         }
     }
