@@ -183,6 +183,14 @@ __device__ __forceinline__ int scan_lanes(int v)
     return v;
 }
 
+// Workgroups go round the eight XCDs one by one: so that the heads of an XCD share keys (and its L2 holds them), it takes
+// neighbours.  8192 rows, 32 heads on 4: the keys and values of one head of 2 MB each in an L2 of 4 MB, not of four.
+__device__ __forceinline__ int att_head(int block, int heads)
+{
+    const int b = block % heads;
+    return heads % 8 ? b : b % 8 * (heads / 8) + b / 8;
+}
+
 struct AttTile {
     int start, len, index;          // first row and length of the sequence, which tile of it
 };

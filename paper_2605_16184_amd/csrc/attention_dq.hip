@@ -22,7 +22,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     constexpr int TILE = DqShape<T, DP, NA, NB, DIRECT>::TILE;
     T *lk = reinterpret_cast<T *>(lds), *lv = lk + TILE;
     AttTile tile;
-    const int head = (int)blockIdx.x % a.heads, kvh = head / a.group;
+    const int head = att_head((int)blockIdx.x, a.heads), kvh = head / a.group;
     if (!find_tile<32 * NA>(a, (int)blockIdx.x / a.heads, tile)) return;
     const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
