@@ -3,8 +3,10 @@ torch tensors on the GPU, build the host descriptor arrays and pass raw pointers
 computed here, and there is no fallback: a missing library is an ImportError."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+import struct
 from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p, POINTER, Structure
 from typing import Optional, Sequence
 
@@ -193,19 +195,19 @@ def lib():
             fn.restype = c_int
             fn.argtypes = [POINTER(_SymPair), c_int, c_void_p]
         L.asteria_dropout.restype = c_int
-        L.asteria_dropout.argtypes = [POINTER(_Drop), POINTER(_Rng), c_void_p]
+        L.asteria_dropout.argtypes = [c_void_p, c_void_p, c_void_p]
         L.asteria_rms_norm.restype = c_int
-        L.asteria_rms_norm.argtypes = [POINTER(_Norm), c_float, POINTER(_Rng), c_void_p]
+        L.asteria_rms_norm.argtypes = [c_void_p, c_float, c_void_p, c_void_p]
         L.asteria_rms_norm_backward_workspace_bytes.restype = c_size_t
-        L.asteria_rms_norm_backward_workspace_bytes.argtypes = [POINTER(_NormGrad)]
+        L.asteria_rms_norm_backward_workspace_bytes.argtypes = [c_void_p]
         L.asteria_rms_norm_backward.restype = c_int
-        L.asteria_rms_norm_backward.argtypes = [POINTER(_NormGrad), c_float, POINTER(_Rng), c_void_p, c_size_t, c_void_p]
+        L.asteria_rms_norm_backward.argtypes = [c_void_p, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
         L.asteria_attention.restype = c_int
-        L.asteria_attention.argtypes = [POINTER(_Attn), c_void_p]
+        L.asteria_attention.argtypes = [c_void_p, c_void_p]
         L.asteria_attention_backward_workspace_bytes.restype = c_size_t
-        L.asteria_attention_backward_workspace_bytes.argtypes = [POINTER(_Attn)]
+        L.asteria_attention_backward_workspace_bytes.argtypes = [c_void_p]
         L.asteria_attention_backward.restype = c_int
-        L.asteria_attention_backward.argtypes = [POINTER(_Attn), POINTER(_AttnGrad), c_void_p, c_size_t, c_void_p]
+        L.asteria_attention_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         L.asteria_profile_i8_flops.restype = c_int
         L.asteria_profile_i8_flops.argtypes = [POINTER(ctypes.c_double)]
         L.asteria_profile_root_work.restype = c_int
@@ -641,68 +643,95 @@ def sym_unpack(items, stream=None) -> None:
 
 
 # ---------------------------------------------------------------------------- operators of a decoder layer
+#
+# These calls are short (a few microseconds on the device), so the host's part counts: descriptors are packed in one go, sizes and
+# devices of a tensor read once, and the raw handle of the current stream is taken.
 
-class _On:
-    """The device of a call's tensors, which must be one, made current, and the stream the call is enqueued on: ``stream``, or
-    the device's current one.  Workspaces are allocated on that stream, so that their memory is free for others only behind it."""
+_RNG = struct.Struct("@QQQf0Q")
+_DROP = struct.Struct("@QQ5i0Q")
+_NORM = struct.Struct("@6Q11i0Q")
+_NORM_GRAD = struct.Struct("@7Q11i0Q")
+_ATTN = struct.Struct("@6Q8q6if0Q")
+_ATTN_GRAD = struct.Struct("@4Q8q")
+_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+_E4M3 = torch.float8_e4m3fn
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
-    def __init__(self, stream, *tensors):
-        dev = tensors[0].device
-        for t in tensors:
-            if t is not None and (t.device != dev or not t.is_cuda):
-                raise ValueError("need GPU tensors on one device")
-        if stream is not None and stream.device != dev:
-            raise ValueError("the stream belongs to another device than the tensors")
-        self.device, self.given = dev, stream
-        self.guard = None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        self.stream = c_void_p((self.given or torch.cuda.current_stream(self.device)).cuda_stream)
-        return self
+def _on(stream, *tensors):
+    """(device, raw stream, context) of a call: its tensors lie on one device, which the context makes current where it is not;
+    the stream is the given one or that device's current one."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev or dev < 0:
+            raise ValueError("need GPU tensors on one device")
+    ctx = _HERE_ALREADY if torch.cuda.current_device() == dev else torch.cuda.device(dev)
+    if stream is None:
+        return dev, _raw_stream(dev), ctx
+    if stream.device.index != dev:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return dev, stream.cuda_stream, ctx
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
 
-    def workspace(self, ws, need: int):
-        if ws is None and not need:
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _scratch(ws, need: int, dev: int, stream):
+    """(pointer, bytes) of the workspace.  One that is not given is allocated on the call's stream, so that its memory is free for
+    others only behind it."""
+    if ws is None:
+        if not need:
             return None, 0
-        if ws is None and self.given is not None:
-            with torch.cuda.stream(self.given):
-                ws = _workspace(None, need, self.device)
-        ws = _workspace(ws, need, self.device)
-        if ws.device != self.device:
-            raise ValueError("workspace on another device than the tensors")
-        return c_void_p(ws.data_ptr()), ws.numel()
+        if stream is None:
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        else:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif ws.get_device() != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 GPU tensor on the device of the others")
+    return ws.data_ptr(), ws.numel()
 
 
-def _rng(p, seed, offset, state):
+def _pack_rng(p, seed, offset, state):
     if not p:
         return None
     if not 0.0 <= p < 1.0:
         raise ValueError("p: a probability below 1")
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed, offset: 64-bit numbers")
-    if state is not None and (not state.is_cuda or state.dtype not in (torch.int64, torch.uint64) or state.numel() < 2 or not state.is_contiguous()):
+    if state is None:
+        return _RNG.pack(seed, offset, 0, p)
+    if state.dtype not in (torch.int64, torch.uint64) or state.numel() < 2 or not state.is_contiguous():
         raise ValueError("rng: need a contiguous GPU tensor of two 64-bit numbers (seed, offset)")
-    return _Rng(seed, offset, state.data_ptr() if state is not None else None, p)
+    return _RNG.pack(seed, offset, state.data_ptr(), p)
 
 
-def _as_mat(t, name, shape, dtype=None):
-    """(pointer, leading dimension) of an optional matrix of a given shape."""
-    if t is None:
-        return None, 0
-    ptr, r, c, ld = _mat(t, name, dtype)
-    if (r, c) != shape:
-        raise ValueError(f"{name}: expected {shape}, got {(r, c)}")
-    return ptr, ld
+def _code(t, name):
+    c = _CODE.get(t.dtype)
+    if c is None:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    return c
+
+
+def _rows(t, name, shape=None, dtype=None):
+    """(pointer, leading dimension) of a matrix with unit column stride, of a given shape and dtype."""
+    s, st = t.shape, t.stride()
+    if len(s) != 2 or st[1] != 1 and s[1] > 1:
+        raise ValueError(f"{name}: need a 2-D tensor with unit column stride")
+    if shape is not None and s != shape:
+        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(s)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    return t.data_ptr(), st[0] if s[0] > 1 else max(s[1], st[0])
+
+
+def _rows_or_none(t, name, shape, dtype=None):
+    return (0, 0) if t is None else _rows(t, name, shape, dtype)
 
 
 def _vec(t, name, n):
     if t is None:
-        return None
+        return 0
     if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{name}: need a contiguous vector of {n} elements")
     return t.data_ptr()
@@ -713,13 +742,15 @@ def dropout(X: torch.Tensor, Y: torch.Tensor, p: float, seed: int = 0, offset: i
     """Y = X with elements dropped with probability p (a multiple of 2^-16), the others times 1 / (1 - p); Y may be X.  Which ones is
     a function of (seed, offset) and of the element's row and column alone: the same call on a gradient is the backward pass.
     ``rng``: GPU tensor of two 64-bit numbers (seed, offset), read when the kernel runs, instead of the arguments."""
-    with _On(stream, X, Y, rng) as on:
-        d = _Drop()
-        d.X, d.rows, d.cols, d.ldx = _mat(X, "X")
-        d.dtype = _dtype_code(X)
-        d.Y, d.ldy = _as_mat(Y, "Y", (d.rows, d.cols), X.dtype)
-        r = _rng(p, seed, offset, rng) or _Rng(0, 0, None, 0.0)
-        _check(lib().asteria_dropout(ctypes.byref(d), ctypes.byref(r), on.stream), "asteria_dropout")
+    _, raw, ctx = _on(stream, X, Y, rng)
+    shape = X.shape
+    x, ldx = _rows(X, "X")
+    y, ldy = _rows(Y, "Y", shape, X.dtype)
+    d = _DROP.pack(x, y, shape[0], shape[1], ldx, ldy, _code(X, "X"))
+    r = _pack_rng(p, seed, offset, rng) or _RNG.pack(0, 0, 0, 0.0)
+    with ctx:
+        st = lib().asteria_dropout(d, r, raw)
+    _check(st, "asteria_dropout")
 
 
 def rms_norm(X: torch.Tensor, Y: torch.Tensor, W: Optional[torch.Tensor] = None, R: Optional[torch.Tensor] = None,
@@ -727,50 +758,45 @@ def rms_norm(X: torch.Tensor, Y: torch.Tensor, W: Optional[torch.Tensor] = None,
              p: float = 0.0, seed: int = 0, offset: int = 0, rng: Optional[torch.Tensor] = None, stream=None) -> None:
     """H = R + dropout(X), Y = H W / sqrt(mean(H^2) + eps) per row.  R, W, H may be None (zero, ones, not written).  Y of dtype
     float8_e4m3fn: Y = y / scale with fp32 ``scale`` (rows x 1, or rows x ceil(cols / 128) with ``group`` = 128)."""
-    with _On(stream, X, Y, W, R, H, scale, rng) as on:
-        n = _Norm()
-        n.X, n.rows, n.cols, n.ldx = _mat(X, "X")
-        shape = (n.rows, n.cols)
-        n.x_dtype = _dtype_code(X)
-        n.R, n.ldr = _as_mat(R, "R", shape)
-        n.H, n.ldh = _as_mat(H, "H", shape)
-        if R is not None and H is not None and R.dtype != H.dtype:
-            raise TypeError("R and H must be of one dtype")
-        ref = R if R is not None else H
-        n.h_dtype = _dtype_code(ref) if ref is not None else F32
-        n.Y, n.ldy = _as_mat(Y, "Y", shape)
-        n.y_dtype = E4M3 if Y.dtype == torch.float8_e4m3fn else _dtype_code(Y)
-        n.W, n.w_dtype = _vec(W, "W", n.cols), F32 if W is None else _dtype_code(W)
-        n.group = int(group)
-        if scale is not None:
-            groups = -(-n.cols // 128) if group else 1
-            if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != n.rows * groups:
-                raise ValueError(f"scale: need a contiguous fp32 tensor of {n.rows} x {groups} elements")
-            n.Scale = scale.data_ptr()
-        r = _rng(p, seed, offset, rng)
-        _check(lib().asteria_rms_norm(ctypes.byref(n), float(eps), ctypes.byref(r) if r else None, on.stream), "asteria_rms_norm")
+    _, raw, ctx = _on(stream, X, Y, W, R, H, scale, rng)
+    shape = X.shape
+    x, ldx = _rows(X, "X")
+    rows, cols = shape
+    r_, ldr = _rows_or_none(R, "R", shape)
+    h, ldh = _rows_or_none(H, "H", shape, None if R is None else R.dtype)
+    ref = R if R is not None else H
+    y, ldy = _rows(Y, "Y", shape)
+    sc = 0
+    if scale is not None:
+        if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != rows * (-(-cols // 128) if group else 1):
+            raise ValueError(f"scale: need a contiguous fp32 tensor of {rows} x {-(-cols // 128) if group else 1} elements")
+        sc = scale.data_ptr()
+    n = _NORM.pack(x, r_, _vec(W, "W", cols), h, y, sc, rows, cols, ldx, ldr, ldh, ldy, _code(X, "X"),
+                   F32 if ref is None else _code(ref, "R, H"), E4M3 if Y.dtype == _E4M3 else _code(Y, "Y"),
+                   F32 if W is None else _code(W, "W"), group)
+    r = _pack_rng(p, seed, offset, rng)
+    with ctx:
+        st = lib().asteria_rms_norm(n, eps, r, raw)
+    _check(st, "asteria_rms_norm")
 
 
-def _norm_grad(H, dY, W, dH, dX, dR, dW):
-    n = _NormGrad()
-    n.H, n.rows, n.cols, n.ldh = _mat(H, "H")
-    shape = (n.rows, n.cols)
-    n.h_dtype = _dtype_code(H)
-    n.dY, n.lddy = _as_mat(dY, "dY", shape)
-    n.y_dtype = _dtype_code(dY)
-    n.dH, n.lddh = _as_mat(dH, "dH", shape, H.dtype)
-    n.dR, n.lddr = _as_mat(dR, "dR", shape, H.dtype)
-    n.dX, n.lddx = _as_mat(dX, "dX", shape)
-    n.x_dtype = F32 if dX is None else _dtype_code(dX)
+def _pack_norm_grad(H, dY, W, dH, dX, dR, dW):
+    shape, dt = H.shape, H.dtype
+    h, ldh = _rows(H, "H")
+    rows, cols = shape
+    dy, lddy = _rows(dY, "dY", shape)
+    dh, lddh = _rows_or_none(dH, "dH", shape, dt)
+    dx, lddx = _rows_or_none(dX, "dX", shape)
+    dr, lddr = _rows_or_none(dR, "dR", shape, dt)
     if W is not None and dW is not None and W.dtype != dW.dtype:
         raise TypeError("W and dW must be of one dtype")
     ref = W if W is not None else dW
-    n.W, n.dW, n.w_dtype = _vec(W, "W", n.cols), _vec(dW, "dW", n.cols), F32 if ref is None else _dtype_code(ref)
-    return n
+    return _NORM_GRAD.pack(h, dy, _vec(W, "W", cols), dh, dx, dr, _vec(dW, "dW", cols), rows, cols, ldh, lddy, lddh, lddx, lddr,
+                           F32 if dX is None else _code(dX, "dX"), _code(H, "H"), _code(dY, "dY"), F32 if ref is None else _code(ref, "W"))
 
 
 def rms_norm_backward_workspace_bytes(H, dY, W=None, dH=None, dX=None, dR=None, dW=None) -> int:
-    return lib().asteria_rms_norm_backward_workspace_bytes(ctypes.byref(_norm_grad(H, dY, W, dH, dX, dR, dW)))
+    return lib().asteria_rms_norm_backward_workspace_bytes(_pack_norm_grad(H, dY, W, dH, dX, dR, dW))
 
 
 def rms_norm_backward(H: torch.Tensor, dY: torch.Tensor, W: Optional[torch.Tensor] = None, dH: Optional[torch.Tensor] = None,
@@ -779,47 +805,50 @@ def rms_norm_backward(H: torch.Tensor, dY: torch.Tensor, W: Optional[torch.Tenso
                       ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """Gradients of rms_norm at the stored sum H: dR = dH + the norm's gradient of dY, dX = dropout(dR) with the forward pass's
     random numbers, dW.  dH (in) and each of dX, dR, dW (out) may be None."""
-    with _On(stream, H, dY, W, dH, dX, dR, dW, rng) as on:
-        n = _norm_grad(H, dY, W, dH, dX, dR, dW)
-        r = _rng(p, seed, offset, rng)
-        ptr, size = on.workspace(ws, lib().asteria_rms_norm_backward_workspace_bytes(ctypes.byref(n)))
-        _check(lib().asteria_rms_norm_backward(ctypes.byref(n), float(eps), ctypes.byref(r) if r else None, ptr, size, on.stream),
-               "asteria_rms_norm_backward")
+    dev, raw, ctx = _on(stream, H, dY, W, dH, dX, dR, dW, rng)
+    n = _pack_norm_grad(H, dY, W, dH, dX, dR, dW)
+    r = _pack_rng(p, seed, offset, rng)
+    L = lib()
+    ptr, size = _scratch(ws, L.asteria_rms_norm_backward_workspace_bytes(n) if ws is None else 0, dev, stream)
+    with ctx:
+        st = L.asteria_rms_norm_backward(n, eps, r, ptr, size, raw)
+    _check(st, "asteria_rms_norm_backward")
 
 
-def _heads(t, name, dtype=None, shape=None):
+def _heads(t, name, shape=None, dtype=None):
     """(pointer, row stride, head stride) of a rows x heads x dim tensor."""
-    if t.dim() != 3 or t.stride(2) != 1 and t.shape[2] > 1:
+    s, st = t.shape, t.stride()
+    if len(s) != 3 or st[2] != 1 and s[2] > 1:
         raise ValueError(f"{name}: need a 3-D tensor (rows, heads, dim) with unit stride along dim")
+    if shape is not None and s != shape:
+        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(s)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), st[0], st[1]
 
 
-def _attn(Q, K, V, O, lse, cu, scale):
-    a = _Attn()
-    if Q.dim() != 3 or K.dim() != 3:
-        raise ValueError("Q, K: need 3-D tensors (rows, heads, dim)")
-    a.total, a.heads, a.dim = Q.shape
-    a.kv_heads = K.shape[1]
-    a.dtype = _dtype_code(Q)
-    a.Q, a.ldq, a.hq = _heads(Q, "Q")
-    a.K, a.ldk, a.hk = _heads(K, "K", Q.dtype, (a.total, a.kv_heads, a.dim))
-    a.V, a.ldv, a.hv = _heads(V, "V", Q.dtype, (a.total, a.kv_heads, a.dim))
-    a.O, a.ldo, a.ho = _heads(O, "O", Q.dtype, (a.total, a.heads, a.dim))
+def _pack_attn(Q, K, V, O, lse, cu, scale):
+    shape, kv_shape, dt = Q.shape, K.shape, Q.dtype
+    q, ldq, hq = _heads(Q, "Q")
+    k, ldk, hk = _heads(K, "K", None, dt)
+    total, heads, dim = shape
+    if kv_shape[0] != total or kv_shape[2] != dim:
+        raise ValueError(f"K: expected {total} rows and dim {dim}, got {tuple(kv_shape)}")
+    v, ldv, hv = _heads(V, "V", kv_shape, dt)
+    o, ldo, ho = _heads(O, "O", shape, dt)
+    ls = 0
     if lse is not None:
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (a.heads, a.total) or not lse.is_contiguous():
-            raise ValueError(f"lse: need a contiguous fp32 tensor of {a.heads} x {a.total} elements")
-        a.lse = lse.data_ptr()
-    a.nseq = 1
+        if lse.dtype != torch.float32 or lse.shape != (heads, total) or not lse.is_contiguous():
+            raise ValueError(f"lse: need a contiguous fp32 tensor of {heads} x {total} elements")
+        ls = lse.data_ptr()
+    c, nseq = 0, 1
     if cu is not None:
         if cu.dtype != torch.int32 or cu.dim() != 1 or cu.shape[0] < 2 or not cu.is_contiguous():
             raise ValueError("cu: need a contiguous int32 GPU tensor of the sequences' first rows and the end")
-        a.cu, a.nseq = cu.data_ptr(), cu.shape[0] - 1
-    a.scale = a.dim ** -0.5 if scale is None and a.dim else scale or 0.0
-    return a
+        c, nseq = cu.data_ptr(), cu.shape[0] - 1
+    if scale is None:
+        scale = dim ** -0.5 if dim else 1.0
+    return _ATTN.pack(q, k, v, o, ls, c, ldq, ldk, ldv, ldo, hq, hk, hv, ho, total, nseq, heads, kv_shape[1], dim, _code(Q, "Q"), scale)
 
 
 def attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, lse: Optional[torch.Tensor] = None,
@@ -827,25 +856,31 @@ def attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor
     """O = softmax(scale Q K^T, causal within every sequence) V.  Q, O: rows x heads x dim; K, V: rows x kv_heads x dim; sequence s is
     rows cu[s] .. cu[s + 1] - 1 (``cu``: int32 GPU tensor; None: all rows are one sequence); rows of no sequence are left as they
     are.  ``lse`` (heads x rows, fp32): what the backward pass needs.  ``scale``: default dim^-1/2."""
-    with _On(stream, Q, K, V, O, lse, cu) as on:
-        a = _attn(Q, K, V, O, lse, cu, scale)
-        _check(lib().asteria_attention(ctypes.byref(a), on.stream), "asteria_attention")
+    _, raw, ctx = _on(stream, Q, K, V, O, lse, cu)
+    a = _pack_attn(Q, K, V, O, lse, cu, scale)
+    with ctx:
+        st = lib().asteria_attention(a, raw)
+    _check(st, "asteria_attention")
 
 
 def attention_backward_workspace_bytes(Q, K, V, O, lse=None, cu=None) -> int:
-    return lib().asteria_attention_backward_workspace_bytes(ctypes.byref(_attn(Q, K, V, O, lse, cu, None)))
+    return lib().asteria_attention_backward_workspace_bytes(_pack_attn(Q, K, V, O, lse, cu, None))
 
 
 def attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor, lse: torch.Tensor, dO: torch.Tensor,
                        dQ: torch.Tensor, dK: torch.Tensor, dV: torch.Tensor, cu: Optional[torch.Tensor] = None,
                        scale: Optional[float] = None, ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """dQ, dK, dV of attention from dO and from the O and lse that attention wrote; rows of no sequence are left as they are."""
-    with _On(stream, Q, K, V, O, lse, dO, dQ, dK, dV, cu) as on:
-        a = _attn(Q, K, V, O, lse, cu, scale)
-        g = _AttnGrad()
-        g.dO, g.lddo, g.hdo = _heads(dO, "dO", Q.dtype, tuple(Q.shape))
-        g.dQ, g.lddq, g.hdq = _heads(dQ, "dQ", Q.dtype, tuple(Q.shape))
-        g.dK, g.lddk, g.hdk = _heads(dK, "dK", Q.dtype, tuple(K.shape))
-        g.dV, g.lddv, g.hdv = _heads(dV, "dV", Q.dtype, tuple(V.shape))
-        ptr, size = on.workspace(ws, lib().asteria_attention_backward_workspace_bytes(ctypes.byref(a)))
-        _check(lib().asteria_attention_backward(ctypes.byref(a), ctypes.byref(g), ptr, size, on.stream), "asteria_attention_backward")
+    dev, raw, ctx = _on(stream, Q, K, V, O, lse, dO, dQ, dK, dV, cu)
+    a = _pack_attn(Q, K, V, O, lse, cu, scale)
+    dt, kv_shape = Q.dtype, K.shape
+    do, lddo, hdo = _heads(dO, "dO", Q.shape, dt)
+    dq, lddq, hdq = _heads(dQ, "dQ", Q.shape, dt)
+    dk, lddk, hdk = _heads(dK, "dK", kv_shape, dt)
+    dv, lddv, hdv = _heads(dV, "dV", kv_shape, dt)
+    g = _ATTN_GRAD.pack(do, dq, dk, dv, lddo, lddq, lddk, lddv, hdo, hdq, hdk, hdv)
+    L = lib()
+    ptr, size = _scratch(ws, L.asteria_attention_backward_workspace_bytes(a) if ws is None else 0, dev, stream)
+    with ctx:
+        st = L.asteria_attention_backward(a, g, ptr, size, raw)
+    _check(st, "asteria_attention_backward")
