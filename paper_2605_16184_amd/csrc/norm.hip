@@ -13,7 +13,7 @@ using namespace asteria;
 
 namespace {
 
-constexpr int MAX_COLS = 16384, MAX_ROWS = 1 << 22;   // 2^22 rows: a workgroup of 1024 threads each
+constexpr int MAX_COLS = 16384, MAX_ROWS = 1 << 22;   // so many workgroups of 512 threads a launch takes
 constexpr float E4M3_MAX = 448.0f, SCALE_FLOOR = 0x1p-100f;
 
 struct NormArgs {
@@ -31,7 +31,7 @@ template <int TPR> constexpr int norm_threads() { return TPR > 256 ? TPR : 256; 
 template <int TPR, int VPT, typename TX, typename TH>
 __global__ __launch_bounds__(norm_threads<TPR>()) void norm_kernel(NormArgs a)
 {
-    __shared__ float part[norm_threads<TPR>() / 64];
+    __shared__ float part[norm_threads<TPR>() / 64][1];
     read_state(a.drop);
     const int t = (int)threadIdx.x % TPR;
     // a wavefront (TPR = 64) or workgroup without a row of its own works on the last one and writes nothing
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < VPT; ++v) r[v].zero();
     }
-    float h[VPT][8], sum = 0.0f;
+    float h[VPT][8], sum[1] = {0.0f};
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
 #pragma unroll
@@ -68,12 +68,13 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_kernel(NormArgs a)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             h[v][e] += r[v].get(e);
-            sum += h[v][e] * h[v][e];
+            sum[0] += h[v][e] * h[v][e];
         }
         const int c = (v * TPR + t) * 8;
         if (live && a.H && c < a.cols) store8(reinterpret_cast<TH *>(a.H) + (size_t)row * a.ldh + c, h[v], a.cols - c);
     }
-    const float rs = 1.0f / sqrtf(row_reduce<false, TPR>(sum, part) / (float)a.cols + a.eps);
+    row_reduce<false, TPR>(sum, part);
+    const float rs = 1.0f / sqrtf(sum[0] / (float)a.cols + a.eps);
     float top[VPT];
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
@@ -98,12 +99,12 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < VPT; ++v) top[v] = lanes_reduce<true, 16>(top[v]);
     } else {
-        float m = top[0];
+        float m[1] = {top[0]};
 #pragma unroll
-        for (int v = 1; v < VPT; ++v) m = fmaxf(m, top[v]);
-        m = row_reduce<true, TPR>(m, part);
+        for (int v = 1; v < VPT; ++v) m[0] = fmaxf(m[0], top[v]);
+        row_reduce<true, TPR>(m, part);
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) top[v] = m;
+        for (int v = 0; v < VPT; ++v) top[v] = m[0];
     }
     if (!live) return;
     const int groups = a.group ? (a.cols + 127) / 128 : 1;
@@ -147,7 +148,7 @@ template <int TPR, int VPT, typename TH, typename TY>
 __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGradArgs a)
 {
     constexpr int NT = norm_threads<TPR>(), RPB = NT / TPR;
-    __shared__ float part[NT / 64];
+    __shared__ float part[NT / 64][2];
     read_state(a.drop);
     const int t = (int)threadIdx.x % TPR;
     float dw[VPT][8];
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGrad
                 if (a.dH) g[v].load(reinterpret_cast<const TH *>(a.dH) + (size_t)row * a.lddh + c, a.cols - c);
             }
         }
-        float n[VPT][8], hh = 0.0f, nh = 0.0f;
+        float n[VPT][8], sums[2] = {0.0f, 0.0f};            // of h^2, of n h
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
             const int c = (v * TPR + t) * 8;
@@ -185,12 +186,13 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGrad
             for (int e = 0; e < 8; ++e) {
                 const float he = h[v].get(e);
                 n[v][e] = y[v].get(e) * w[e];
-                hh += he * he;
-                nh += n[v][e] * he;
+                sums[0] += he * he;
+                sums[1] += n[v][e] * he;
             }
         }
-        const float rs = 1.0f / sqrtf(row_reduce<false, TPR>(hh, part) / (float)a.cols + a.eps);
-        const float f = rs * rs * (row_reduce<false, TPR>(nh, part) / (float)a.cols);
+        row_reduce<false, TPR>(sums, part);
+        const float rs = 1.0f / sqrtf(sums[0] / (float)a.cols + a.eps);
+        const float f = rs * rs * (sums[1] / (float)a.cols);
         if (!live) continue;
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
@@ -213,18 +215,18 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGrad
     if (!a.part) return;
     if constexpr (RPB > 1) {
         // the wavefronts of the workgroup hold the same columns
-        __shared__ float sums[RPB][TPR * 8];
+        __shared__ float share[RPB][TPR * 8];
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sums[threadIdx.x / TPR][e * TPR + t] = dw[v][e];
+            for (int e = 0; e < 8; ++e) share[threadIdx.x / TPR][e * TPR + t] = dw[v][e];
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                dw[v][e] = sums[0][e * TPR + t];
+                dw[v][e] = share[0][e * TPR + t];
 #pragma unroll
-                for (int k = 1; k < RPB; ++k) dw[v][e] += sums[k][e * TPR + t];
+                for (int k = 1; k < RPB; ++k) dw[v][e] += share[k][e * TPR + t];
             }
         }
         if (threadIdx.x >= TPR) return;
@@ -236,24 +238,33 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGrad
     }
 }
 
-// dW = sum of the workgroups' partial sums: 32 columns a workgroup, 32 threads a column.
+// dW = sum of the workgroups' partial sums: 32 columns a workgroup, 32 threads a column, eight loads of a thread in flight.
 __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float *part, int nparts, int cols, void *dW, int w_dtype)
 {
     __shared__ float s[32][33];
     const int c = (int)blockIdx.x * 32 + (int)threadIdx.x % 32, k = (int)threadIdx.x / 32;
     float v = 0.0f;
-    if (c < cols)
-        for (int p = k; p < nparts; p += 32) v += part[(size_t)p * cols + c];
+    if (c < cols) {
+        for (int p = k; p < nparts; p += 256) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p + 32 * i < nparts ? part[(size_t)(p + 32 * i) * cols + c] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += x[i];
+        }
+    }
     s[k][threadIdx.x % 32] = v;
     __syncthreads();
     if (k == 0 && c < cols) {
-        for (int i = 1; i < 32; ++i) v += s[i][threadIdx.x % 32];
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v += s[i][threadIdx.x % 32];
         if (w_dtype == ASTERIA_BF16) reinterpret_cast<uint16_t *>(dW)[c] = f32_bf16(v);
         else reinterpret_cast<float *>(dW)[c] = v;
     }
 }
 
-// Rows of up to 2048 elements take one wavefront, of up to 8192 four, longer ones sixteen.
+// Rows of up to 2048 elements take one wavefront, of up to 8192 four, longer ones eight.
 template <typename F> asteria_status for_width(int cols, F f)
 {
     if (cols <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
@@ -261,13 +272,15 @@ template <typename F> asteria_status for_width(int cols, F f)
     if (cols <= 2048) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
     if (cols <= 4096) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
     if (cols <= 8192) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
 }
 
+// As many workgroups as run at a time (two a CU), each with the same number of rows or one less: every one more is a row of
+// partial sums to write and to read.
 int grad_blocks(int rows, int cols)
 {
-    const int rpb = cols <= 2048 ? 4 : 1, want = (rows + rpb - 1) / rpb;
-    return want < 1024 ? want : 1024;
+    const int rpb = cols <= 2048 ? 4 : 1, units = (rows + rpb - 1) / rpb, per = (units + 511) / 512;
+    return (units + per - 1) / per;
 }
 
 bool valid_eps(float eps) { return eps >= 0.0f && isfinite(eps); }

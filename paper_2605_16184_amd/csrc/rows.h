@@ -156,26 +156,47 @@ __device__ __forceinline__ void drop_chunk(const Dropper &d, uint32_t r, uint32_
 // ---- sums and maxima over the threads of a row -----------------------------------------------------
 template <bool MAX> __device__ __forceinline__ float join(float a, float b) { return MAX ? fmaxf(a, b) : a + b; }
 
+template <int CTRL> __device__ __forceinline__ float dpp(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+
+// Over 16 lanes side by side or the 64 of the wavefront, the result in all of them, without LDS.
 template <bool MAX, int WIDTH> __device__ __forceinline__ float lanes_reduce(float v)
 {
-#pragma unroll
-    for (int o = WIDTH / 2; o > 0; o >>= 1) v = join<MAX>(v, __shfl_xor(v, o));
+    static_assert(WIDTH == 16 || WIDTH == 64, "");
+    v = join<MAX>(v, dpp<0xb1>(v));       // lanes 1 0 3 2 of a quad
+    v = join<MAX>(v, dpp<0x4e>(v));       // lanes 2 3 0 1
+    v = join<MAX>(v, dpp<0x141>(v));      // 7 - i of eight
+    v = join<MAX>(v, dpp<0x140>(v));      // 15 - i of sixteen
+    if constexpr (WIDTH == 64) {
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = join<MAX>(__uint_as_float(a[0]), __uint_as_float(a[1]));
+        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = join<MAX>(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
     return v;
 }
 
-// Over TPR threads (64: one wavefront; more: the workgroup, through `part`, which the call leaves free for the next one).
-template <bool MAX, int TPR> __device__ __forceinline__ float row_reduce(float v, float *part)
+// N values over TPR threads (64: one wavefront; more: the workgroup, through `part`, which the call leaves free for the next one).
+template <bool MAX, int TPR, int N> __device__ __forceinline__ void row_reduce(float (&v)[N], float (*part)[N])
 {
-    v = lanes_reduce<MAX, 64>(v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lanes_reduce<MAX, 64>(v[i]);
     if constexpr (TPR > 64) {
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = part[0];
+        if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-        for (int w = 1; w < TPR / 64; ++w) v = join<MAX>(v, part[w]);
+            for (int i = 0; i < N; ++i) part[threadIdx.x >> 6][i] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = part[0][i];
+#pragma unroll
+            for (int w = 1; w < TPR / 64; ++w) v[i] = join<MAX>(v[i], part[w][i]);
+        }
     }
-    return v;
 }
 
 }  // namespace asteria
