@@ -444,9 +444,17 @@ inline int64_t att_tiles(const AttArgs &a, int qt)
     if (!a.cu) return ((int64_t)a.total + qt - 1) / qt;
     return (int64_t)a.total / qt + (a.nseq < a.total ? a.nseq : a.total);
 }
-// A wavefront for every 32 rows, four of which share a tile of the rows they pass over - or where that gives less than two
-// workgroups a CU, four wavefronts for the same 32 rows, each with a quarter of what is passed over.
-inline bool att_few(const AttArgs &a, int heads) { return att_tiles(a, 128) * heads < 512; }
+// A wavefront for every 32 rows, four of which share a tile of the rows they pass over - or where that gives less than one and a
+// half workgroups a CU, four wavefronts for the same 32 rows, each with a quarter of what is passed over.  Forward and backward, heads of
+// 64: at 324 workgroups 101 us so, 104 us otherwise, at 444 155 and 144 us (bf16); 500 and 540, 855 and 757 us (fp32).
+inline bool att_few(const AttArgs &a, int heads) { return att_tiles(a, 128) * heads < 384; }
+
+// LDS to ask for.  fp32 workgroups that would all run at once, two a CU, are given so much that one has the CU: the longest then
+// do not share one while others stand idle (8192 rows, 8 heads of 64: forward 213 -> 176 us).
+template <typename T, int NB> constexpr size_t att_lds(size_t need, int64_t blocks)
+{
+    return sizeof(T) == 4 && NB == 1 && blocks < 1024 && need < 84 * 1024 ? 84 * 1024 : need;
+}
 
 // Kernels for dims padded to 64, 96 or 128.
 template <typename F> asteria_status att_for_type(int dtype, int dim, bool direct, F f)

@@ -217,10 +217,11 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(AttArgs a)
 template <typename T, int DP, int KB, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)
 {
     static bool configured[MAX_DEVICES] = {};
-    constexpr size_t bytes = DkvShape<T, DP, NA, NB, DIRECT>::LDS;
-    auto kernel = attention_dkv_kernel<T, DP, KB, NA, NB, DIRECT>;
-    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), bytes, configured); e != hipSuccess) return e;
     const int64_t blocks = att_tiles(a, 32 * KB * NA) * (a.heads / a.group) * a.splits;
+    constexpr size_t MOST = att_lds<T, NB>(DkvShape<T, DP, NA, NB, DIRECT>::LDS, 0);
+    const size_t bytes = att_lds<T, NB>(DkvShape<T, DP, NA, NB, DIRECT>::LDS, blocks);
+    auto kernel = attention_dkv_kernel<T, DP, KB, NA, NB, DIRECT>;
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), MOST, configured); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(ATT_THREADS), bytes, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
     const int64_t threads = (int64_t)a.total * (a.heads / a.group) * ((a.dim + 7) / 8);

@@ -114,9 +114,11 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
 template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)
 {
     static bool configured[MAX_DEVICES] = {};
-    constexpr size_t bytes = DqShape<T, DP, NA, NB, DIRECT>::LDS;
-    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(attention_dq_kernel<T, DP, NA, NB, DIRECT>), bytes, configured); e != hipSuccess) return e;
-    hipLaunchKernelGGL((attention_dq_kernel<T, DP, NA, NB, DIRECT>), dim3((unsigned)(att_tiles(a, 32 * NA) * a.heads)), dim3(ATT_THREADS), bytes, stream, a);
+    const int64_t blocks = att_tiles(a, 32 * NA) * a.heads;
+    constexpr size_t MOST = att_lds<T, NB>(DqShape<T, DP, NA, NB, DIRECT>::LDS, 0);
+    const size_t bytes = att_lds<T, NB>(DqShape<T, DP, NA, NB, DIRECT>::LDS, blocks);
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(attention_dq_kernel<T, DP, NA, NB, DIRECT>), MOST, configured); e != hipSuccess) return e;
+    hipLaunchKernelGGL((attention_dq_kernel<T, DP, NA, NB, DIRECT>), dim3((unsigned)blocks), dim3(ATT_THREADS), bytes, stream, a);
     return hipGetLastError();
 }
 
