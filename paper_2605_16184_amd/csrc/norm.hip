@@ -264,9 +264,11 @@ __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float *par
     }
 }
 
-// Rows of up to 2048 elements take one wavefront, of up to 8192 four, longer ones eight.
+// Rows of up to 128 elements take 16 lanes (the norm of queries and keys, a row per head), of up to 2048 one wavefront, of up to
+// 8192 four, longer ones eight.
 template <typename F> asteria_status for_width(int cols, F f)
 {
+    if (cols <= 128) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
     if (cols <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
     if (cols <= 1024) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
     if (cols <= 2048) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
@@ -279,7 +281,7 @@ template <typename F> asteria_status for_width(int cols, F f)
 // partial sums to write and to read.
 int grad_blocks(int rows, int cols)
 {
-    const int rpb = cols <= 2048 ? 4 : 1, units = (rows + rpb - 1) / rpb, per = (units + 511) / 512;
+    const int rpb = cols <= 128 ? 16 : cols <= 2048 ? 4 : 1, units = (rows + rpb - 1) / rpb, per = (units + 511) / 512;
     return (units + per - 1) / per;
 }
 

@@ -178,11 +178,11 @@ template <bool MAX, int WIDTH> __device__ __forceinline__ float lanes_reduce(flo
     return v;
 }
 
-// N values over TPR threads (64: one wavefront; more: the workgroup, through `part`, which the call leaves free for the next one).
+// N values over TPR threads (16, or a wavefront; more: the workgroup, through `part`, which the call leaves free for the next one).
 template <bool MAX, int TPR, int N> __device__ __forceinline__ void row_reduce(float (&v)[N], float (*part)[N])
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lanes_reduce<MAX, 64>(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = lanes_reduce<MAX, TPR < 64 ? TPR : 64>(v[i]);
     if constexpr (TPR > 64) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) {

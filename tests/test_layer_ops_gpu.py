@@ -125,7 +125,7 @@ def _norm_ref(X, R, W, factor, eps):
     return h, h * r * w, size, size * r * w.abs()
 
 
-WIDTHS = [1, 7, 8, 64, 129, 511, 512, 513, 777, 1024, 1025, 2047, 2048, 2049, 4097, 5632, 8193, 16384]
+WIDTHS = [1, 7, 8, 64, 127, 128, 129, 511, 512, 513, 777, 1024, 1025, 2047, 2048, 2049, 4097, 5632, 8193, 16384]
 
 
 @pytest.mark.parametrize("cols", WIDTHS)
@@ -392,6 +392,16 @@ def test_attention_of_heads_and_layouts(heads, kv_heads, layout, dtype):
 @pytest.mark.parametrize("lens", [[5] * 64, [1] * 65 + [300], [0] * 100 + [200, 17] + [0] * 30, [129, 1] * 100])
 def test_attention_of_many_sequences(lens):
     _attention_check(lens, 2, 1, 64, bf16, tail=7)
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("heads,kv_heads", [(64, 16), (48, 48), (96, 2)])
+@pytest.mark.parametrize("lens,dim,layout", [
+    ([129, 257, 31, 300, 64], 64, "packed"), ([129, 257, 0, 300, 64, 1], 64, "odd"), ([400, 127, 128], 128, "packed"),
+    ([385, 2, 250], 128, "odd"), ([300, 300], 96, "heads"), ([97, 480], 80, "packed"), ([280, 150, 33], 33, "packed")])
+def test_attention_of_many_heads(lens, dim, layout, heads, kv_heads, dtype):
+    # enough tiles of 128 rows for all of the chip; heads that share keys dealt to several workgroups
+    _attention_check(lens, heads, kv_heads, dim, dtype, lead=2, tail=4, layout=layout)
 
 
 @pytest.mark.parametrize("scale", [1e-3, 1.0, 4.0])
