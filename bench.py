@@ -41,6 +41,7 @@ MEASURED_F64_MFMA_LOOP = 58.8
 PEAK_HBM = 8000.0       # GB/s
 
 ALL_SECTIONS = ("shampoo", "cpu", "soap", "lowrank", "stress", "staleness")
+ASKED_SECTIONS = ("layer",)     # not in a run that names none
 
 
 def stored_traffic(key: str):
@@ -214,7 +215,7 @@ def main() -> int:
     ap.add_argument("--int8-slices", type=int, default=-1, help="products of the fp64 iterations: -1 = library default (int8 cores, 5 slices), 0 = fp64 cores, 4 | 5")
     ap.add_argument("--schedule", type=int, default=1, help="1 = interval-adapted coefficients, 0 = classical Newton")
     ap.add_argument("--sections", default=",".join(ALL_SECTIONS),
-                    help="comma-separated subset of " + ",".join(ALL_SECTIONS) + " (shampoo always runs)")
+                    help="comma-separated subset of " + ",".join(ALL_SECTIONS) + " (shampoo always runs), or more: " + ",".join(ASKED_SECTIONS))
     ap.add_argument("--soap-groups", type=int, default=2, help="auxiliary streams the SOAP refresh deals its factors to (1..4)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-soap", action="store_true", help="skip the SOAP section (blocks <= 2048)")
@@ -349,6 +350,9 @@ def main() -> int:
         torch.cuda.empty_cache()
     if "stress" in sections:
         out["stress_4096"] = stress_section(args, torch, ast, W, dev)
+        torch.cuda.empty_cache()
+    if "layer" in sections:
+        out["layer"] = layer_section(args, torch, ast, W, dev)
     print(json.dumps(out), flush=True)
     return 0
 
@@ -433,6 +437,57 @@ def lowrank_section(args, torch, ast, W, dev):
             "not_converged": int((res["info"] != 0).sum()),
             "precision_plan": {"fp64_prefix_iters": run.plan[0], "fp16_split_from_iter": run.plan[1]},
             "refresh_mfma": r["refresh_mfma"], "gemm_time_share_ms_per_step": r["gemm_time_share_ms_per_step"]}
+
+
+def layer_section(args, torch, ast, W, dev):
+    """One decoder layer of the 1.1B model on four sequences of 2048 rows, dropout 0.1, bf16 with an fp32 residual stream: its forward
+    and backward pass, the library's operators in it by themselves, and statistics and preconditioned gradients of its blocks."""
+    from paper_2605_16184_amd.layer import DecoderLayer, gradient_blocks
+    rows, p = 8192, 6554 / 65536
+    layer = DecoderLayer(rows, dropout=p, device=dev)
+    cu = torch.arange(0, rows + 1, 2048, dtype=torch.int32, device=dev)
+    r = torch.randn(rows, layer.d, device=dev)
+    dout = torch.randn(rows, layer.d, device=dev) * 1e-3
+    layer.forward(r, cu)
+    _, grads = layer.backward(dout)
+    Gs = gradient_blocks(grads)
+    shapes = [tuple(G.shape) for G in Gs]
+    assert shapes == W.block_shapes([m for m in W.llama_1b_matrices() if m[0].startswith("l0.")], 1024)
+    Ls, Rs = [torch.zeros(m, m, device=dev) for m, _ in shapes], [torch.zeros(n, n, device=dev) for _, n in shapes]
+    XLs, XRs = [torch.empty_like(L) for L in Ls], [torch.empty_like(R) for R in Rs]
+    Ps = [torch.empty(s, device=dev) for s in shapes]
+    info = torch.zeros(2 * len(Gs), dtype=torch.int32, device=dev)
+    blocks, pblocks = ast.Blocks(list(zip(Gs, Ls, Rs))), ast.PBlocks(list(zip(XLs, Gs, XRs, Ps)))
+    ast.stats_update(blocks, 0.95)
+    ast.inverse_root(list(zip(Ls, XLs)) + list(zip(Rs, XRs)), 1e-6, info=info)
+    q, k, v = layer._split(layer._saved[3])
+    dq, dk, dv = layer._split(layer.dqkv)
+    dO = torch.randn_like(layer.O) * 1e-3
+    parts = {
+        "forward": lambda: layer.forward(r, cu),
+        "backward": lambda: layer.backward(dout),
+        "attention": lambda: ast.attention(q, k, v, layer.O, lse=layer.lse, cu=cu),
+        "attention_backward": lambda: ast.attention_backward(q, k, v, layer.O, layer.lse, dO, dq, dk, dv, cu=cu, ws=layer.ws),
+        "rms_norm": lambda: ast.rms_norm(layer.y1, layer.y2, W=layer.norm2, R=r, H=layer.H, p=p, seed=1),
+        "dropout": lambda: ast.dropout(layer.y1, layer.y1, p, seed=1),
+        "stats_update": lambda: ast.stats_update(blocks, 0.95),
+        "precondition": lambda: ast.precondition(pblocks),
+    }
+    out = {"workload": "one decoder layer (2048 wide, 32 heads on 4, FFN 5632), 4 sequences of 2048 rows, dropout 0.1, bf16", "blocks": len(Gs),
+           "not_converged": int((info != 0).sum())}
+    for name, f in parts.items():
+        for _ in range(3): f()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(10): f()
+        b.record()
+        b.synchronize()
+        out[name + "_ms"] = round(a.elapsed_time(b) / 10, 4)
+    pairs = 4 * 2048 * 2049 // 2
+    for name, products in (("attention", 2), ("attention_backward", 5)):
+        out[name + "_tflops"] = round(2 * products * pairs * layer.d / out[name + "_ms"] / 1e9, 1)
+    log(f"[bench] layer: {out}")
+    return out
 
 
 def stress_section(args, torch, ast, W, dev):

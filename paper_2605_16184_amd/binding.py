@@ -3,7 +3,6 @@ torch tensors on the GPU, build the host descriptor arrays and pass raw pointers
 computed here, and there is no fallback: a missing library is an ImportError."""
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import struct
@@ -655,25 +654,35 @@ _ATTN = struct.Struct("@6Q8q6if0Q")
 _ATTN_GRAD = struct.Struct("@4Q8q")
 _CODE = {torch.float32: F32, torch.bfloat16: BF16}
 _E4M3 = torch.float8_e4m3fn
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _on(stream, *tensors):
-    """(device, raw stream, context) of a call: its tensors lie on one device, which the context makes current where it is not;
+def _on(stream, first, *tensors):
+    """(device, raw stream, device to go back to) of a call: its tensors lie on one device, which is made current where it is not;
     the stream is the given one or that device's current one."""
-    dev = tensors[0].get_device()
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("need GPU tensors")
     for t in tensors:
-        if t is not None and t.get_device() != dev or dev < 0:
+        if t is not None and t.get_device() != dev:
             raise ValueError("need GPU tensors on one device")
-    ctx = _HERE_ALREADY if torch.cuda.current_device() == dev else torch.cuda.device(dev)
     if stream is None:
-        return dev, _raw_stream(dev), ctx
-    if stream.device.index != dev:
+        raw = _raw_stream(dev)
+    elif stream.device.index == dev:
+        raw = stream.cuda_stream
+    else:
         raise ValueError("the stream belongs to another device than the tensors")
-    return dev, stream.cuda_stream, ctx
+    return dev, raw, None if _current_device() == dev else torch.cuda.device(dev)
 
 
-_HERE_ALREADY = contextlib.nullcontext()
+def _enqueue(where, f, ctx, *args):
+    if ctx is None:
+        st = f(*args)
+    else:
+        with ctx:
+            st = f(*args)
+    if st:
+        raise AsteriaError(st, where)
 
 
 def _scratch(ws, need: int, dev: int, stream):
@@ -714,19 +723,21 @@ def _code(t, name):
 
 
 def _rows(t, name, shape=None, dtype=None):
-    """(pointer, leading dimension) of a matrix with unit column stride, of a given shape and dtype."""
-    s, st = t.shape, t.stride()
-    if len(s) != 2 or st[1] != 1 and s[1] > 1:
-        raise ValueError(f"{name}: need a 2-D tensor with unit column stride")
-    if shape is not None and s != shape:
+    """(pointer, leading dimension) of a matrix with unit column stride, of a given shape and dtype; of None: (0, 0)."""
+    if t is None:
+        return 0, 0
+    s = t.shape
+    if shape is None:
+        if len(s) != 2:
+            raise ValueError(f"{name}: need a 2-D tensor")
+    elif s != shape:
         raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(s)}")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    return t.data_ptr(), st[0] if s[0] > 1 else max(s[1], st[0])
-
-
-def _rows_or_none(t, name, shape, dtype=None):
-    return (0, 0) if t is None else _rows(t, name, shape, dtype)
+    ld, one = t.stride()
+    if one != 1 and s[1] > 1:
+        raise ValueError(f"{name}: need unit column stride")
+    return t.data_ptr(), ld if s[0] > 1 else max(s[1], ld)
 
 
 def _vec(t, name, n):
@@ -748,9 +759,7 @@ def dropout(X: torch.Tensor, Y: torch.Tensor, p: float, seed: int = 0, offset: i
     y, ldy = _rows(Y, "Y", shape, X.dtype)
     d = _DROP.pack(x, y, shape[0], shape[1], ldx, ldy, _code(X, "X"))
     r = _pack_rng(p, seed, offset, rng) or _RNG.pack(0, 0, 0, 0.0)
-    with ctx:
-        st = lib().asteria_dropout(d, r, raw)
-    _check(st, "asteria_dropout")
+    _enqueue("asteria_dropout", lib().asteria_dropout, ctx, d, r, raw)
 
 
 def rms_norm(X: torch.Tensor, Y: torch.Tensor, W: Optional[torch.Tensor] = None, R: Optional[torch.Tensor] = None,
@@ -762,8 +771,8 @@ def rms_norm(X: torch.Tensor, Y: torch.Tensor, W: Optional[torch.Tensor] = None,
     shape = X.shape
     x, ldx = _rows(X, "X")
     rows, cols = shape
-    r_, ldr = _rows_or_none(R, "R", shape)
-    h, ldh = _rows_or_none(H, "H", shape, None if R is None else R.dtype)
+    r_, ldr = _rows(R, "R", shape)
+    h, ldh = _rows(H, "H", shape, None if R is None else R.dtype)
     ref = R if R is not None else H
     y, ldy = _rows(Y, "Y", shape)
     sc = 0
@@ -775,9 +784,7 @@ def rms_norm(X: torch.Tensor, Y: torch.Tensor, W: Optional[torch.Tensor] = None,
                    F32 if ref is None else _code(ref, "R, H"), E4M3 if Y.dtype == _E4M3 else _code(Y, "Y"),
                    F32 if W is None else _code(W, "W"), group)
     r = _pack_rng(p, seed, offset, rng)
-    with ctx:
-        st = lib().asteria_rms_norm(n, eps, r, raw)
-    _check(st, "asteria_rms_norm")
+    _enqueue("asteria_rms_norm", lib().asteria_rms_norm, ctx, n, eps, r, raw)
 
 
 def _pack_norm_grad(H, dY, W, dH, dX, dR, dW):
@@ -785,9 +792,9 @@ def _pack_norm_grad(H, dY, W, dH, dX, dR, dW):
     h, ldh = _rows(H, "H")
     rows, cols = shape
     dy, lddy = _rows(dY, "dY", shape)
-    dh, lddh = _rows_or_none(dH, "dH", shape, dt)
-    dx, lddx = _rows_or_none(dX, "dX", shape)
-    dr, lddr = _rows_or_none(dR, "dR", shape, dt)
+    dh, lddh = _rows(dH, "dH", shape, dt)
+    dx, lddx = _rows(dX, "dX", shape)
+    dr, lddr = _rows(dR, "dR", shape, dt)
     if W is not None and dW is not None and W.dtype != dW.dtype:
         raise TypeError("W and dW must be of one dtype")
     ref = W if W is not None else dW
@@ -810,21 +817,23 @@ def rms_norm_backward(H: torch.Tensor, dY: torch.Tensor, W: Optional[torch.Tenso
     r = _pack_rng(p, seed, offset, rng)
     L = lib()
     ptr, size = _scratch(ws, L.asteria_rms_norm_backward_workspace_bytes(n) if ws is None else 0, dev, stream)
-    with ctx:
-        st = L.asteria_rms_norm_backward(n, eps, r, ptr, size, raw)
-    _check(st, "asteria_rms_norm_backward")
+    _enqueue("asteria_rms_norm_backward", L.asteria_rms_norm_backward, ctx, n, eps, r, ptr, size, raw)
 
 
 def _heads(t, name, shape=None, dtype=None):
     """(pointer, row stride, head stride) of a rows x heads x dim tensor."""
-    s, st = t.shape, t.stride()
-    if len(s) != 3 or st[2] != 1 and s[2] > 1:
-        raise ValueError(f"{name}: need a 3-D tensor (rows, heads, dim) with unit stride along dim")
-    if shape is not None and s != shape:
+    s = t.shape
+    if shape is None:
+        if len(s) != 3:
+            raise ValueError(f"{name}: need a 3-D tensor (rows, heads, dim)")
+    elif s != shape:
         raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(s)}")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    return t.data_ptr(), st[0], st[1]
+    ld, hs, one = t.stride()
+    if one != 1 and s[2] > 1:
+        raise ValueError(f"{name}: need unit stride along dim")
+    return t.data_ptr(), ld, hs
 
 
 def _pack_attn(Q, K, V, O, lse, cu, scale):
@@ -858,9 +867,7 @@ def attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor
     are.  ``lse`` (heads x rows, fp32): what the backward pass needs.  ``scale``: default dim^-1/2."""
     _, raw, ctx = _on(stream, Q, K, V, O, lse, cu)
     a = _pack_attn(Q, K, V, O, lse, cu, scale)
-    with ctx:
-        st = lib().asteria_attention(a, raw)
-    _check(st, "asteria_attention")
+    _enqueue("asteria_attention", lib().asteria_attention, ctx, a, raw)
 
 
 def attention_backward_workspace_bytes(Q, K, V, O, lse=None, cu=None) -> int:
@@ -881,6 +888,4 @@ def attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: tor
     g = _ATTN_GRAD.pack(do, dq, dk, dv, lddo, lddq, lddk, lddv, hdo, hdq, hdk, hdv)
     L = lib()
     ptr, size = _scratch(ws, L.asteria_attention_backward_workspace_bytes(a) if ws is None else 0, dev, stream)
-    with ctx:
-        st = L.asteria_attention_backward(a, g, ptr, size, raw)
-    _check(st, "asteria_attention_backward")
+    _enqueue("asteria_attention_backward", L.asteria_attention_backward, ctx, a, g, ptr, size, raw)
