@@ -9,8 +9,7 @@
 //   forward        S^T = K Q^T,  O^T += V^T P^T             a lane holds one query; V^T read from LDS with transposing loads
 //   gradient of Q  S^T = K Q^T,  dP^T = V dO^T,  dQ^T += K^T dS^T
 //   of K and V     S = Q K^T,  dP = dO V^T,  dV^T += dO^T P,  dK^T += Q^T dS     a lane holds one key
-// In bf16 a product takes v_mfma_f32_32x32x16_bf16; in fp32 the same eight values a lane go through eight
-// v_mfma_f32_32x32x2_f32, each of which takes the pair of places that the two halves of the wavefront hold.
+// All products run on v_mfma_f32_32x32x16_bf16: bf16 operands as they are, fp32 operands in three terms.
 #pragma once
 #include <math.h>
 #include <type_traits>
@@ -34,26 +33,22 @@ constexpr int ATT_THREADS = 256;      // four wavefronts, NA along the tile that
 __device__ __forceinline__ uint32_t lds_place(const void *p) { return (uint32_t)reinterpret_cast<uintptr_t>(p); }
 
 // ---- operands -----------------------------------------------------------------------------------
-// Tiles of rows in LDS.  rows(): eight elements of one row, 8 h .. of the 16 from d on; cols(): of column d + l % 32 the eight rows
+// Operands from tiles of rows in LDS.  rows(): eight elements of one row, 8 h .. of the 16 from d on; cols(): of column d + l % 32 the eight rows
 // 4 h + j % 4 + 8 (j / 4) from r on - the order in which a 32 x 32 result holds its rows.
 template <typename T, int DP> struct Op;
 
-// Rows of whole 16-byte pieces without padding: piece c of row r lies at place c ^ swz(r).  LDS serves 256 bytes a cycle: reads of
-// one piece from 16 rows side by side, and transposing reads of four pieces side by side from four rows, both meet every
-// bank once.  All four bits of r that count change the place by exclusive or, so that one offset a lane serves all reads.
-template <int DP> struct Op<bf16_elem, DP> {
-    typedef bf16_elem T;
-    typedef __bf16 frag __attribute__((ext_vector_type(8)));
-    static constexpr int BLOCKS = 2;          // blocks of 32 staged rows a wavefront takes at a time
-    static constexpr int PITCH = DP > 64 ? 128 : 64;
-    __device__ static __forceinline__ int swz(int r) { return (PITCH == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) + ((r >> 2) & 3); }
-    __device__ static __forceinline__ int place(int r, int c) { return r * PITCH + ((c ^ swz(r)) << 3); }
-    __device__ static __forceinline__ acc16 mma(frag a, frag b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+// Tiles of bf16 rows of P (64 or 128) elements, S elements apart (P, or three times that), without padding: piece c (16 bytes) of row r lies
+// at place c ^ swz(r).  LDS serves 256 bytes a cycle: reads of one piece from 16 rows side by side, and transposing reads of four
+// pieces side by side from four rows, both meet every bank once.
+template <int P, int S> struct Swizzled {
+    typedef __bf16 piece __attribute__((ext_vector_type(8)));
+    __device__ static __forceinline__ int swz(int r) { return (P == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) + ((r >> 2) & 3); }
+    __device__ static __forceinline__ int place(int r, int c) { return r * S + ((c ^ swz(r)) << 3); }
     // What a lane reads of a tile (at a multiple of 256 bytes): the exclusive or with d goes last, on the address, so that it takes
     // one instruction a read and no register over the loop.
     struct Tile {
         uint32_t r, c;
-        __device__ __forceinline__ explicit Tile(const T *tile)
+        __device__ __forceinline__ explicit Tile(const void *tile)
         {
             const int l = (int)threadIdx.x & 63, i = l & 15;
             const uint32_t at = lds_place(tile);
@@ -61,79 +56,106 @@ template <int DP> struct Op<bf16_elem, DP> {
             c = at + 2 * (place(4 * (l >> 5) + (i >> 2), 2 * ((l >> 4) & 1) + ((i & 3) >> 1)) + 4 * (i & 1));
         }
     };
-    // r a multiple of 32, d of 16
-    __device__ static __forceinline__ frag rows(const Tile &t, int r, int d)
+    // r a multiple of 32, d of 16; `more`: elements from the tile's beginning
+    __device__ static __forceinline__ piece rows(const Tile &t, int r, int d, int more = 0)
     {
-        return *reinterpret_cast<__attribute__((address_space(3))) const frag *>((t.r ^ (2 * d)) + r * PITCH * 2);
+        return *reinterpret_cast<__attribute__((address_space(3))) const piece *>((t.r ^ (2 * d)) + (r * S + more) * 2);
     }
     // r a multiple of 16, d of 32: a 16-lane group reads four rows of 16 elements and gets, lane by lane, the columns
-    __device__ static __forceinline__ frag cols(const Tile &t, int r, int d)
+    __device__ static __forceinline__ piece cols(const Tile &t, int r, int d, int more = 0)
     {
-        union { struct { s16x4 lo, hi; } s; frag f; } u;
-        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((t.c ^ (2 * d)) + r * PITCH * 2));
-        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((t.c ^ (2 * d + 32)) + (r + 8) * PITCH * 2));   // swz(r + 8) = swz(r) ^ 2
+        union { struct { s16x4 lo, hi; } s; piece f; } u;
+        u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((t.c ^ (2 * d)) + (r * S + more) * 2));
+        u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>((t.c ^ (2 * d + 32)) + ((r + 8) * S + more) * 2));   // swz(r + 8) = swz(r) ^ 2
         return u.f;
     }
-    __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c) { *reinterpret_cast<u16x8 *>(tile + place(r, d >> 3)) = c.a; }
-    __device__ static __forceinline__ frag pack(const acc16 &v, int from)
+};
+
+template <int DP> struct Op<bf16_elem, DP> {
+    typedef bf16_elem T;
+    static constexpr int BLOCKS = 2;          // blocks of 32 staged rows a wavefront takes at a time
+    static constexpr int PITCH = DP > 64 ? 128 : 64;
+    typedef Swizzled<PITCH, PITCH> Places;
+    typedef typename Places::piece frag;
+    typedef frag held;                        // the operand that stays in registers
+    typedef typename Places::Tile Tile;
+    __device__ static __forceinline__ acc16 mma(const frag &a, const held &b, acc16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    __device__ static __forceinline__ frag rows(const Tile &t, int r, int d) { return Places::rows(t, r, d); }
+    __device__ static __forceinline__ frag cols(const Tile &t, int r, int d) { return Places::cols(t, r, d); }
+    __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c) { *reinterpret_cast<u16x8 *>(tile + Places::place(r, d >> 3)) = c.a; }
+    __device__ static __forceinline__ held pack(const acc16 &v, int from)
     {
-        frag f;
+        held f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = (__bf16)v[from + j];
         return f;
     }
-    __device__ static __forceinline__ float get(const frag &f, int j) { return (float)f[j]; }
-    __device__ static __forceinline__ frag of(const Chunk<T> &c) { return __builtin_bit_cast(frag, c.a); }
+    __device__ static __forceinline__ held of(const Chunk<T> &c) { return __builtin_bit_cast(held, c.a); }
 };
 
-// Rows padded by one piece: reads of a piece from eight rows side by side meet every bank once.  The fp32 matrix cores take 16 times
-// as long as the bf16 ones, so nothing else counts here.
+// fp32: every operand as three bf16 terms, x = hi + mid + lo with the rest below 2^-27 of x, and of the nine products the six above
+// 2^-26: six instructions of 32 cycles where the fp32 matrix cores take eight of 64 for the same 16 places, and the sums are fp32.  A
+// tile is cut once, on its way to LDS, where the terms of a row lie one behind the other (cut by every wavefront that reads it, the
+// vector units were the bound: 580 us instead of 475 us a forward pass of 8192 rows, 16 heads of 128).  An infinite element has no such terms:
+// it counts as no number.
 template <int DP> struct Op<float, DP> {
     typedef float T;
-    typedef float frag __attribute__((ext_vector_type(8)));
-    static constexpr int BLOCKS = 2;
-    static constexpr int PITCH = DP + 4;
-    __device__ static __forceinline__ acc16 mma(frag a, frag b, acc16 c)
+    static constexpr int BLOCKS = DP > 64 ? 1 : 2;
+    static constexpr int P = DP > 64 ? 128 : 64, PITCH = 3 * P / 2;      // PITCH in floats
+    typedef Swizzled<P, 3 * P> Places;
+    typedef typename Places::piece term;
+    struct held { term hi, mid, lo; };
+    typedef held frag;
+    typedef typename Places::Tile Tile;
+    __device__ static __forceinline__ held cut(float (&r)[8])
     {
+        held t;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-        return c;
-    }
-    typedef const T *Tile;
-    __device__ static __forceinline__ frag rows(const T *tile, int r, int d)
-    {
-        const int l = (int)threadIdx.x & 63;
-        const T *p = tile + (r + (l & 31)) * PITCH + d + 8 * (l >> 5);
-        const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
-        return frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    }
-    __device__ static __forceinline__ frag cols(const T *tile, int r, int d)
-    {
-        const int l = (int)threadIdx.x & 63;
-        frag f;
+        for (int j = 0; j < 8; ++j) { t.hi[j] = (__bf16)r[j]; r[j] -= (float)t.hi[j]; }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = tile[(r + 4 * (l >> 5) + (j & 3) + 8 * (j >> 2)) * PITCH + d + (l & 31)];
-        return f;
+        for (int j = 0; j < 8; ++j) { t.mid[j] = (__bf16)r[j]; r[j] -= (float)t.mid[j]; }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t.lo[j] = (__bf16)r[j];
+        return t;
+    }
+    __device__ static __forceinline__ acc16 mma(const frag &a, const held &b, acc16 c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.lo, b.hi, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.hi, b.lo, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.mid, b.mid, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.mid, b.hi, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.hi, b.mid, c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.hi, b.hi, c, 0, 0, 0);
+    }
+    __device__ static __forceinline__ frag rows(const Tile &t, int r, int d)
+    {
+        return frag{Places::rows(t, r, d), Places::rows(t, r, d, P), Places::rows(t, r, d, 2 * P)};
+    }
+    __device__ static __forceinline__ frag cols(const Tile &t, int r, int d)
+    {
+        return frag{Places::cols(t, r, d), Places::cols(t, r, d, P), Places::cols(t, r, d, 2 * P)};
     }
     __device__ static __forceinline__ void put(T *tile, int r, int d, const Chunk<T> &c)
     {
-        *reinterpret_cast<f32x4 *>(tile + r * PITCH + d) = c.a;
-        *reinterpret_cast<f32x4 *>(tile + r * PITCH + d + 4) = c.b;
+        const held t = of(c);
+        term *p = reinterpret_cast<term *>(reinterpret_cast<__bf16 *>(tile) + Places::place(r, d >> 3));
+        p[0] = t.hi;
+        p[P / 8] = t.mid;
+        p[2 * P / 8] = t.lo;
     }
-    __device__ static __forceinline__ frag pack(const acc16 &v, int from)
+    __device__ static __forceinline__ held pack(const acc16 &v, int from)
     {
-        frag f;
+        float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = v[from + j];
-        return f;
+        return cut(f);
     }
-    __device__ static __forceinline__ float get(const frag &f, int j) { return f[j]; }
-    __device__ static __forceinline__ frag of(const Chunk<T> &c)
+    __device__ static __forceinline__ held of(const Chunk<T> &c)
     {
-        frag f;
+        float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = c.get(j);
-        return f;
+        return cut(f);
     }
 };
 
@@ -264,8 +286,7 @@ template <int QT> __device__ __forceinline__ bool find_tile(const AttArgs &a, in
 template <typename T, int DP, int BK, bool DIRECT> struct AttStage;
 
 template <typename T, int DP, int BK> struct AttStage<T, DP, BK, false> {
-    static constexpr int CH = BK * DP / 8 / ATT_THREADS;
-    static_assert(CH * ATT_THREADS * 8 == BK * DP, "whole chunks");
+    static constexpr int ALL = BK * DP / 8, CH = (ALL + ATT_THREADS - 1) / ATT_THREADS;
     Chunk<T> c[CH];
     // rows row0 .. row0 + rows - 1 of one head
     __device__ __forceinline__ void load(const AttArray &a, int row0, int head, int rows, int dim)
@@ -274,7 +295,7 @@ template <typename T, int DP, int BK> struct AttStage<T, DP, BK, false> {
         for (int i = 0; i < CH; ++i) {
             const int k = (int)threadIdx.x + ATT_THREADS * i, r = k / (DP / 8), d = k % (DP / 8) * 8;
             c[i].zero();
-            if (r < rows && d < dim) c[i].load(att_at<const T>(a, row0 + r, head) + d, dim - d);
+            if (r < rows && d < dim && (ALL % ATT_THREADS == 0 || k < ALL)) c[i].load(att_at<const T>(a, row0 + r, head) + d, dim - d);
         }
     }
     __device__ __forceinline__ void store(T *lds) const
@@ -282,7 +303,7 @@ template <typename T, int DP, int BK> struct AttStage<T, DP, BK, false> {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int k = (int)threadIdx.x + ATT_THREADS * i, r = k / (DP / 8), d = k % (DP / 8) * 8;
-            Op<T, DP>::put(lds, r, d, c[i]);
+            if (ALL % ATT_THREADS == 0 || k < ALL) Op<T, DP>::put(lds, r, d, c[i]);
         }
     }
 };
@@ -309,7 +330,7 @@ template <int DP, int BK> struct AttStage<bf16_elem, DP, BK, true> {
     {
         int t = (int)threadIdx.x;
         if constexpr (SPARE) asm("" : "+v"(t));
-        const int r = t / CPR, c = (t % CPR) ^ M::swz(r);
+        const int r = t / CPR, c = (t % CPR) ^ M::Places::swz(r);
         const uint32_t at = c * 8 < dim ? (uint32_t)(r * ld + c * 16) : 0x80000000u;
         const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_place(stage) + (threadIdx.x & ~63u) * 16u);
 #pragma unroll
@@ -345,7 +366,7 @@ inline bool att_direct(const AttArray &a, int dtype, int total, int dim)
 
 // The second operand of a product over dim: lane l holds row `row` of the array, elements 16 c + 8 h + j.
 template <typename T, int DP>
-__device__ __forceinline__ void load_frags(const AttArray &a, int row, int head, bool valid, int dim, typename Op<T, DP>::frag (&f)[DP / 16])
+__device__ __forceinline__ void load_frags(const AttArray &a, int row, int head, bool valid, int dim, typename Op<T, DP>::held (&f)[DP / 16])
 {
     const int h = ((int)threadIdx.x >> 5) & 1;
 #pragma unroll
@@ -360,15 +381,20 @@ __device__ __forceinline__ void load_frags(const AttArray &a, int row, int head,
 
 // The loads of f have arrived behind this: left to their first use, which lies in the loop over the tiles, the wait for them would
 // hold up every step until the next tile's loads have arrived, too.
+template <typename F> __device__ __forceinline__ void arrived(F &f)
+{
+    if constexpr (sizeof(F) == 16) {
+        i32x4 v = __builtin_bit_cast(i32x4, f);
+        asm volatile("" : "+v"(v));
+        f = __builtin_bit_cast(F, v);
+    } else {
+        arrived(f.hi); arrived(f.mid); arrived(f.lo);
+    }
+}
 template <typename F, int N> __device__ __forceinline__ void arrived(F (&f)[N])
 {
-    typedef int words __attribute__((ext_vector_type(sizeof(F) / 4)));
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        words v = __builtin_bit_cast(words, f[i]);
-        asm volatile("" : "+v"(v));
-        f[i] = __builtin_bit_cast(F, v);
-    }
+    for (int i = 0; i < N; ++i) arrived(f[i]);
 }
 
 // Elements 32 t + 8 g + 4 h + 0 .. 3 of the row at p (of dim elements), times f.
@@ -445,9 +471,15 @@ inline int64_t att_tiles(const AttArgs &a, int qt)
     return (int64_t)a.total / qt + (a.nseq < a.total ? a.nseq : a.total);
 }
 // A wavefront for every 32 rows, four of which share a tile of the rows they pass over - or where that gives less than one and a
-// half workgroups a CU, four wavefronts for the same 32 rows, each with a quarter of what is passed over.  Forward and backward, heads of
+// half workgroups a CU, four wavefronts (or two) for the same 32 rows, each with a quarter (half) of what is passed over.  Forward and backward, heads of
 // 64: at 324 workgroups 101 us so, 104 us otherwise, at 444 155 and 144 us (bf16); 500 and 540, 855 and 757 us (fp32).
 inline bool att_few(const AttArgs &a, int heads) { return att_tiles(a, 128) * heads < 384; }
+
+// How many wavefronts the same rows take then.  Tiles of 32 rows for each of them lie in LDS: fp32 ones fill it with two (and a tile that
+// one wavefront reads is cut for it alone: 3200 rows, 12 heads of 64, 397 + 128 us with four, 236 + 69 us with two).
+template <typename T> constexpr int att_shared = sizeof(T) == 4 ? 2 : 4;
+// The last 16 columns of fp32 heads of 65 to 80, which are padding only, are left out of the products over dim (a head of 80: 3 %).
+template <typename T, int DP> __device__ __forceinline__ bool att_empty(int d, int dim) { return sizeof(T) == 4 && DP == 96 && d == 5 && dim <= 80; }
 
 // LDS to ask for.  fp32 workgroups that would all run at once, two a CU, are given so much that one has the CU: the longest then
 // do not share one while others stand idle (8192 rows, 8 heads of 64: forward 213 -> 176 us).

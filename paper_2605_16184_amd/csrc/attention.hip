@@ -14,7 +14,7 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct FwdShape {
 };
 
 template <typename T, int DP, int NA, int NB, bool DIRECT>
-__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention_kernel(AttArgs a)
+__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attention_kernel(AttArgs a)
 {
     typedef Op<T, DP> M;
     constexpr int BK = FwdShape<T, DP, NA, NB, DIRECT>::BK, NBLK = BK / 32 / NB;
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
-    typename M::frag q[DP / 16];
+    typename M::held q[DP / 16];
     load_frags<T, DP>(a.Q, tile.start + qi, head, valid, a.dim, q);
     acc16 o[DP / 32];
 #pragma unroll
@@ -76,9 +76,11 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
 #pragma unroll
         for (int b = 0; b < NBLK; ++b) s[b] = 0.0f;
 #pragma unroll
-        for (int d = 0; d < DP / 16; ++d)
+        for (int d = 0; d < DP / 16; ++d) {
+            if (att_empty<T, DP>(d, a.dim)) break;
 #pragma unroll
             for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s[b]);
+        }
         if (k0 + 32 * NBLK - 1 > qw) {
 #pragma unroll
             for (int b = 0; b < NBLK; ++b)
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const typename M::frag p = M::pack(s[b], 8 * k);
+                const typename M::held p = M::pack(s[b], 8 * k);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tv, 32 * b + 16 * k, 32 * t), p, o[t]);
             }
@@ -207,7 +209,7 @@ extern "C" asteria_status asteria_attention(const asteria_attn *a, void *stream_
         typedef decltype(t) T;
         constexpr int DP = dp();
         constexpr bool DIRECT = decltype(direct_)::value;
-        ASTERIA_HIP_TRY((att_few(k, k.heads) ? launch<T, DP, 1, 4, DIRECT>(k, stream) : launch<T, DP, 4, 1, DIRECT>(k, stream)));
+        ASTERIA_HIP_TRY((att_few(k, k.heads) ? launch<T, DP, 4 / att_shared<T>, att_shared<T>, DIRECT>(k, stream) : launch<T, DP, 4, 1, DIRECT>(k, stream)));
         return ASTERIA_OK;
     });
 }

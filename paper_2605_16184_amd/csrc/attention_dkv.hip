@@ -40,7 +40,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
     tile.index = (tile.len + KT - 1) / KT - 1 - tile.index;      // the first keys are seen by the most rows
     const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
     const int kw = tile.index * KT + wa * 32 * KB, ki = kw + (l & 31);
-    typename M::frag kf[KB][DP / 16], vf[KB][DP / 16];
+    typename M::held kf[KB][DP / 16], vf[KB][DP / 16];
     acc16 dk[KB][DP / 32], dv[KB][DP / 32];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -49,10 +49,10 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) { dk[kb][t] = 0.0f; dv[kb][t] = 0.0f; }
     }
-    typedef typename M::frag frag;
+    typedef typename M::held piece;
     constexpr int HELD = Shape::HELD, REGS = DP / 16 - HELD;
     static_assert(HELD == 0 || KB == 1, "one block of keys");
-    frag *held = reinterpret_cast<frag *>(rows_of(STAGES)) + w * HELD * 64 + l;
+    piece *held = reinterpret_cast<piece *>(rows_of(STAGES)) + w * HELD * 64 + l;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) held[64 * i] = vf[0][REGS + i];
     const float c = a.scale * LOG2E;
@@ -125,6 +125,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
             }
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
+                if (att_empty<T, DP>(d, a.dim)) break;
                 const typename M::frag q = M::rows(tq, 32 * b, 16 * d), g = M::rows(tg, 32 * b, 16 * d);
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                typename M::frag p[KB], ds[KB];
+                typename M::held p[KB], ds[KB];
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) { p[kb] = M::pack(s[kb], 8 * k); ds[kb] = M::pack(dp[kb], 8 * k); }
 #pragma unroll
@@ -248,7 +249,7 @@ asteria_status asteria::attention_dkv(const AttArgs &a, int dtype, hipStream_t s
         typedef decltype(t) T;
         constexpr int DP = dp();
         constexpr bool DIRECT = decltype(direct_)::value;
-        ASTERIA_HIP_TRY((att_few(a, a.heads / a.group * a.splits) ? launch<T, DP, 1, 1, 4, DIRECT>(a, stream)
+        ASTERIA_HIP_TRY((att_few(a, a.heads / a.group * a.splits) ? launch<T, DP, 1, 4 / att_shared<T>, att_shared<T>, DIRECT>(a, stream)
                                                                    : launch<T, DP, 1, 4, 1, DIRECT>(a, stream)));
         return ASTERIA_OK;
     });

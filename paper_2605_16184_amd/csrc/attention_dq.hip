@@ -14,7 +14,7 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct DqShape {
 };
 
 template <typename T, int DP, int NA, int NB, bool DIRECT>
-__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttArgs a)
+__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attention_dq_kernel(AttArgs a)
 {
     typedef Op<T, DP> M;
     constexpr int BK = DqShape<T, DP, NA, NB, DIRECT>::BK;
@@ -27,14 +27,22 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
     const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
-    typename M::frag q[DP / 16], g[DP / 16];
+    typename M::held q[DP / 16], g[DP / 16];
     float delta = 0.0f;
-    load_frags<T, DP>(a.O, tile.start + qi, head, valid, a.dim, q);
-    load_frags<T, DP>(a.dO, tile.start + qi, head, valid, a.dim, g);
 #pragma unroll
-    for (int d = 0; d < DP / 16; ++d)
+    for (int d = 0; d < DP / 16; ++d) {
+        const int at = 16 * d + 8 * h;
+        Chunk<T> o, go;
+        o.zero();
+        go.zero();
+        if (valid && at < a.dim) {
+            o.load(att_at<T>(a.O, tile.start + qi, head) + at, a.dim - at);
+            go.load(att_at<T>(a.dO, tile.start + qi, head) + at, a.dim - at);
+        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) delta += M::get(q[d], j) * M::get(g[d], j);
+        for (int j = 0; j < 8; ++j) delta += o.get(j) * go.get(j);
+        g[d] = M::of(go);
+    }
     delta = join_halves<false>(delta);
     const size_t at_row = (size_t)head * a.total + tile.start + qi;
     const float lse_ = valid ? a.lse[at_row] : 0.0f, lse = lse_ * LOG2E;
@@ -89,6 +97,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
             acc16 s = 0.0f, dp = from;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
+                if (att_empty<T, DP>(d, a.dim)) break;
                 s = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s);
                 dp = M::mma(M::rows(tv, 32 * b, 16 * d), g[d], dp);
             }
@@ -101,7 +110,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 ? 2 : 1) void attention
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const typename M::frag p = M::pack(s, 8 * k);
+                const typename M::held p = M::pack(s, 8 * k);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tk, 32 * b + 16 * k, 32 * t), p, o[t]);
             }
@@ -131,7 +140,7 @@ asteria_status asteria::attention_dq(const AttArgs &a, int dtype, hipStream_t st
         typedef decltype(t) T;
         constexpr int DP = dp();
         constexpr bool DIRECT = decltype(direct_)::value;
-        ASTERIA_HIP_TRY((att_few(a, a.heads) ? launch<T, DP, 1, 4, DIRECT>(a, stream) : launch<T, DP, 4, 1, DIRECT>(a, stream)));
+        ASTERIA_HIP_TRY((att_few(a, a.heads) ? launch<T, DP, 4 / att_shared<T>, att_shared<T>, DIRECT>(a, stream) : launch<T, DP, 4, 1, DIRECT>(a, stream)));
         return ASTERIA_OK;
     });
 }
