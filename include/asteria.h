@@ -521,7 +521,7 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i, dP = dO V^T, dS = P (dP - D):
  *   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dK and dV summed over the heads that share them,
  * without atomics: every run gives the same bits.
- * Errors: NULL pointers, sizes <= 0, heads no multiple of kv_heads, bad dtype, scale not positive and finite, negative strides,
+ * Errors: NULL pointers, sizes <= 0, heads no multiple of kv_heads, bad dtype, scale not within 2^-100 .. 2^100, negative strides,
  * written arrays that overlap themselves, cu NULL with nseq > 1 -> INVALID_ARG; dim > 128, or (total / 128 + nseq) heads >= 2^24 -> UNSUPPORTED. */
 typedef struct asteria_attn {
     const void *Q, *K, *V;

@@ -170,7 +170,7 @@ asteria_status validate(const asteria_attn *a, bool writes_o)
     if (!a || !a->Q || !a->K || !a->V || !a->O) return ASTERIA_INVALID_ARG;
     if (a->total <= 0 || a->nseq <= 0 || a->heads <= 0 || a->kv_heads <= 0 || a->dim <= 0) return ASTERIA_INVALID_ARG;
     if (a->heads % a->kv_heads || (!a->cu && a->nseq != 1) || !valid_dtype(a->dtype)) return ASTERIA_INVALID_ARG;
-    if (!(a->scale > 0.0f) || !isfinite(a->scale)) return ASTERIA_INVALID_ARG;
+    if (!(a->scale >= 0x1p-100f && a->scale <= 0x1p100f)) return ASTERIA_INVALID_ARG;      // lse / scale and 8 / scale are numbers
     if (a->ldq < 0 || a->ldk < 0 || a->ldv < 0 || a->ldo < 0 || a->hq < 0 || a->hk < 0 || a->hv < 0 || a->ho < 0) return ASTERIA_INVALID_ARG;
     if (writes_o && !apart(a->ldo, a->ho, a->total, a->heads, a->dim)) return ASTERIA_INVALID_ARG;
     if (a->dim > 128) return ASTERIA_UNSUPPORTED;

@@ -106,7 +106,7 @@ GRAD = {"dO": 0x7000, "dQ": 0x8000, "dK": 0x9000, "dV": 0xa000, "lddo": 32, "hdo
 
 @pytest.mark.parametrize("bad", [
     {"Q": None}, {"K": None}, {"V": None}, {"O": None}, {"total": 0}, {"nseq": 0}, {"heads": 0}, {"kv_heads": 0}, {"dim": 0}, {"kv_heads": 3},
-    {"cu": None}, {"dtype": 2}, {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"ldq": -1}, {"hk": -8}])
+    {"cu": None}, {"dtype": 2}, {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"scale": 2.0 ** -101}, {"scale": 2.0 ** 101}, {"ldq": -1}, {"hk": -8}])
 def test_attention_refuses_bad_arguments(bad):
     lib = ast.lib()
     assert lib.asteria_attention(_make(B._Attn, ATTN, bad), None) == B.INVALID_ARG
