@@ -475,6 +475,35 @@ def test_attention_scores_of_the_lowest_values():
     assert float(torch.linalg.norm(O[:40, 0].double() - mean) / torch.linalg.norm(mean)) <= 1e-5
 
 
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("heads", [1, 192])
+def test_attention_scores_that_rise_and_fall(heads, dtype):
+    # no score to go by for several tiles, then scores of -500, then steps up by hundreds and down again, at places within tiles
+    n = 700
+    Q, K, V = torch.zeros(n, heads, 64, device=DEV), torch.zeros(n, 1, 64, device=DEV), _randn(n, 1, 64, seed=3)
+    Q[:, :, 0] = 1.0
+    K[:, 0, 0] = -3e38
+    K[:, 0, 1] = -3e38
+    Q[:, :, 1] = 1.0                                        # the sum of both passes the range: minus infinity
+    K[210:, 0, 1] = 0.0
+    K[210:, 0, 0] = -500.0
+    K[333:, 0, 0] = -100.0
+    K[350:, 0, 0] = -480.0
+    K[420:, 0, 0] = 300.0
+    K[421:, 0, 0] = 304.0
+    K[640:, 0, 0] = 295.0
+    Q, K, V = Q.to(dtype), K.to(dtype), V.to(dtype)
+    O, lse = torch.empty_like(Q), torch.empty(heads, n, device=DEV)
+    ast.attention(Q, K, V, O, lse=lse, scale=1.0)
+    z = K[210:, 0, 0].double().expand(n - 210, n - 210)
+    z = torch.where(torch.ones(n - 210, n - 210, device=DEV).tril().bool(), z, -math.inf)
+    ref = torch.softmax(z, 1) @ V[210:, 0].double()
+    tol = (U[dtype] * 1.01 + (U[bf16] * 1.01 if dtype == bf16 else 0.0) + 2 * 504 * 4 * F + 1000 * F) * (torch.softmax(z, 1) @ V[210:, 0].double().abs())
+    for j in (0, heads - 1):
+        _inside(O[210:, j], ref, tol, "O")
+        _inside(lse[j, 210:], torch.logsumexp(z, 1), torch.full((n - 210,), 504 * 8 * F, dtype=torch.float64, device=DEV), "lse")
+
+
 def test_attention_gradient_against_differences():
     # of the forward pass in 64 bits, along one random direction of all three inputs
     Q, K, V, dO = (_randn(130, h, 40, seed=i) for i, h in enumerate((4, 2, 2, 4)))
