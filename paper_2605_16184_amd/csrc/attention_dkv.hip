@@ -1,4 +1,4 @@
-// Gradients of K and V (attention.h): a wavefront holds the keys and values of 32 KB rows in registers and passes over the
+// Gradients of K and V (attention.h): a wavefront holds the keys and values of 32 rows in registers and passes over the
 // rows that see them, in all the heads that share them.
 //
 // Where the heads that share keys are many and the tiles are few, several workgroups take a part of these heads each, leave
@@ -21,12 +21,12 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct DkvShape {
     static constexpr size_t LDS = STAGED > SUMS ? STAGED : SUMS;
 };
 
-template <typename T, int DP, int KB, int NA, int NB, bool DIRECT>
+template <typename T, int DP, int NA, int NB, bool DIRECT>
 __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT) ? 2 : 1) void attention_dkv_kernel(AttArgs a)
 {
     typedef Op<T, DP> M;
     typedef DkvShape<T, DP, NA, NB, DIRECT> Shape;
-    constexpr int BQ = Shape::BQ, KT = 32 * KB * NA;
+    constexpr int BQ = Shape::BQ, KT = 32 * NA;
     extern __shared__ __attribute__((aligned(256))) char lds[];
     constexpr int STAGES = DIRECT ? 2 : 1;
     constexpr bool FROM = sizeof(T) == 2;
@@ -39,22 +39,18 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
     const int per = a.group / a.splits, head0 = kvh * a.group + split * per;
     tile.index = (tile.len + KT - 1) / KT - 1 - tile.index;      // the first keys are seen by the most rows
     const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
-    const int kw = tile.index * KT + wa * 32 * KB, ki = kw + (l & 31);
-    typename M::held kf[KB][DP / 16], vf[KB][DP / 16];
-    acc16 dk[KB][DP / 32], dv[KB][DP / 32];
+    const int kw = tile.index * KT + wa * 32, ki = kw + (l & 31);
+    typename M::held kf[DP / 16], vf[DP / 16];
+    acc16 dk[DP / 32], dv[DP / 32];
+    load_frags<T, DP>(a.K, tile.start + ki, kvh, ki < tile.len, a.dim, kf);
+    load_frags<T, DP>(a.V, tile.start + ki, kvh, ki < tile.len, a.dim, vf);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-        load_frags<T, DP>(a.K, tile.start + ki + 32 * kb, kvh, ki + 32 * kb < tile.len, a.dim, kf[kb]);
-        load_frags<T, DP>(a.V, tile.start + ki + 32 * kb, kvh, ki + 32 * kb < tile.len, a.dim, vf[kb]);
-#pragma unroll
-        for (int t = 0; t < DP / 32; ++t) { dk[kb][t] = 0.0f; dv[kb][t] = 0.0f; }
-    }
+    for (int t = 0; t < DP / 32; ++t) { dk[t] = 0.0f; dv[t] = 0.0f; }
     typedef typename M::held piece;
     constexpr int HELD = Shape::HELD, REGS = DP / 16 - HELD;
-    static_assert(HELD == 0 || KB == 1, "one block of keys");
     piece *held = reinterpret_cast<piece *>(rows_of(STAGES)) + w * HELD * 64 + l;
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) held[64 * i] = vf[0][REGS + i];
+    for (int i = 0; i < HELD; ++i) held[64 * i] = vf[REGS + i];
     const float c = a.scale * LOG2E;
     const int first = tile.index * KT / BQ, nq = (tile.len + BQ - 1) / BQ;
     AttStage<T, DP, BQ, DIRECT> sq, sg;
@@ -86,8 +82,8 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
     const int steps = (nq - first) * per;
     int qt = first, head = head0;
     load(head, qt * BQ, 0);
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) { arrived(kf[kb]); arrived(vf[kb]); }
+    arrived(kf);
+    arrived(vf);
     for (int step = 0; step < steps; ++step) {
         const int q0 = qt * BQ, stage = DIRECT ? step & 1 : 0;
         lq = reinterpret_cast<T *>(lds) + stage * 2 * Shape::TILE;
@@ -113,80 +109,61 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 && (DP == 64 || DIRECT)
             if (qb + 31 < kw) continue;                 // rows before this wavefront's keys
             // the sums begin at -lse / scale and at -D of their rows: one instruction an element less each.  In bf16, where P is rounded to
             // 2^-8 anyway: dim additions on top of a large lse cost fp32 results up to three bits (measured at scores around 100)
-            acc16 s[KB], dp[KB];
+            acc16 s, dp;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 rl = *reinterpret_cast<const f32x4 *>(row_lse + 32 * b + 8 * g + 4 * h);
                 const f32x4 rd = *reinterpret_cast<const f32x4 *>(row_delta + 32 * b + 8 * g + 4 * h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) { s[kb][4 * g + e] = FROM ? rl[e] : 0.0f; dp[kb][4 * g + e] = FROM ? rd[e] : 0.0f; }
+                for (int e = 0; e < 4; ++e) { s[4 * g + e] = FROM ? rl[e] : 0.0f; dp[4 * g + e] = FROM ? rd[e] : 0.0f; }
             }
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
                 if (att_empty<T, DP>(d, a.dim)) break;
                 const typename M::frag q = M::rows(tq, 32 * b, 16 * d), g = M::rows(tg, 32 * b, 16 * d);
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) {
-                    s[kb] = M::mma(q, kf[kb][d], s[kb]);
-                    dp[kb] = M::mma(g, d < REGS ? vf[kb][d] : held[64 * (d - REGS)], dp[kb]);
-                }
+                s = M::mma(q, kf[d], s);
+                dp = M::mma(g, d < REGS ? vf[d] : held[64 * (d - REGS)], dp);
             }
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+            for (int i = 0; i < 16; ++i) {
+                const int r = 32 * b + acc_row(i, h);
+                s[i] = __builtin_amdgcn_exp2f(FROM ? s[i] * c : __builtin_fmaf(s[i], c, row_lse[r] * c));
+                dp[i] = s[i] * (FROM ? dp[i] : dp[i] + row_delta[r]);
+            }
+            if (qb < kw + 31) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int r = 32 * b + acc_row(i, h);
-                    s[kb][i] = __builtin_amdgcn_exp2f(FROM ? s[kb][i] * c : __builtin_fmaf(s[kb][i], c, row_lse[r] * c));
-                    dp[kb][i] = s[kb][i] * (FROM ? dp[kb][i] : dp[kb][i] + row_delta[r]);
+                    const int r = qb + acc_row(i, h);
+                    if (r < ki) s[i] = 0.0f;
+                    if (r < ki || r == 0) dp[i] = 0.0f;    // row 0: as in the gradient of Q
                 }
-            if (qb < kw + 32 * KB - 1) {
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = qb + acc_row(i, h);
-                        if (r < ki + 32 * kb) s[kb][i] = 0.0f;
-                        if (r < ki + 32 * kb || r == 0) dp[kb][i] = 0.0f;    // row 0: as in the gradient of Q
-                    }
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                typename M::held p[KB], ds[KB];
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) { p[kb] = M::pack(s[kb], 8 * k); ds[kb] = M::pack(dp[kb], 8 * k); }
+                const typename M::held p = M::pack(s, 8 * k), ds = M::pack(dp, 8 * k);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) {
                     const typename M::frag g = M::cols(tg, 32 * b + 16 * k, 32 * t), q = M::cols(tq, 32 * b + 16 * k, 32 * t);
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) {
-                        dv[kb][t] = M::mma(g, p[kb], dv[kb][t]);
-                        dk[kb][t] = M::mma(q, ds[kb], dk[kb][t]);
-                    }
+                    dv[t] = M::mma(g, p, dv[t]);
+                    dk[t] = M::mma(q, ds, dk[t]);
                 }
             }
         }
     }
     if constexpr (NB > 1) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), dk[kb]);
-            add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), dv[kb]);
-        }
+        add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), dk);
+        add_wavefronts<DP, NA, NB>(reinterpret_cast<float *>(lds), dv);
         if (wb) return;
     }
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-        if (ki + 32 * kb >= tile.len) continue;
-        const int row = tile.start + ki + 32 * kb;
+    if (ki < tile.len) {
+        const int row = tile.start + ki;
         if (a.part) {
             float *p = a.part + (((size_t)split * a.total + row) * kv_heads + kvh) * a.dim;
-            store_row<float, DP>(p, a.dim, dk[kb], 1.0f);
-            store_row<float, DP>(p + (size_t)a.splits * a.total * kv_heads * a.dim, a.dim, dv[kb], 1.0f);
+            store_row<float, DP>(p, a.dim, dk, 1.0f);
+            store_row<float, DP>(p + (size_t)a.splits * a.total * kv_heads * a.dim, a.dim, dv, 1.0f);
         } else {
-            store_row<T, DP>(att_at<T>(a.dK, row, kvh), a.dim, dk[kb], a.scale);
-            store_row<T, DP>(att_at<T>(a.dV, row, kvh), a.dim, dv[kb], 1.0f);
+            store_row<T, DP>(att_at<T>(a.dK, row, kvh), a.dim, dk, a.scale);
+            store_row<T, DP>(att_at<T>(a.dV, row, kvh), a.dim, dv, 1.0f);
         }
     }
 }
@@ -215,13 +192,13 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(AttArgs a)
     store8(att_at<T>(blockIdx.y == 0 ? a.dK : a.dV, row, kvh) + d, sum, a.dim - d);
 }
 
-template <typename T, int DP, int KB, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)
+template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)
 {
     static bool configured[MAX_DEVICES] = {};
-    const int64_t blocks = att_tiles(a, 32 * KB * NA) * (a.heads / a.group) * a.splits;
+    const int64_t blocks = att_tiles(a, 32 * NA) * (a.heads / a.group) * a.splits;
     constexpr size_t MOST = att_lds<T, NB>(DkvShape<T, DP, NA, NB, DIRECT>::LDS, 0);
     const size_t bytes = att_lds<T, NB>(DkvShape<T, DP, NA, NB, DIRECT>::LDS, blocks);
-    auto kernel = attention_dkv_kernel<T, DP, KB, NA, NB, DIRECT>;
+    auto kernel = attention_dkv_kernel<T, DP, NA, NB, DIRECT>;
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), MOST, configured); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(ATT_THREADS), bytes, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
@@ -249,8 +226,8 @@ asteria_status asteria::attention_dkv(const AttArgs &a, int dtype, hipStream_t s
         typedef decltype(t) T;
         constexpr int DP = dp();
         constexpr bool DIRECT = decltype(direct_)::value;
-        ASTERIA_HIP_TRY((att_few(a, a.heads / a.group * a.splits) ? launch<T, DP, 1, 4 / att_shared<T>, att_shared<T>, DIRECT>(a, stream)
-                                                                   : launch<T, DP, 1, 4, 1, DIRECT>(a, stream)));
+        ASTERIA_HIP_TRY((att_few(a, a.heads / a.group * a.splits) ? launch<T, DP, 4 / att_shared<T>, att_shared<T>, DIRECT>(a, stream)
+                                                                   : launch<T, DP, 4, 1, DIRECT>(a, stream)));
         return ASTERIA_OK;
     });
 }
