@@ -91,8 +91,9 @@ class DecoderLayer:
         B.rms_norm_backward(self.H, dy2, W=self.norm2, dH=dout, dX=da, dR=dH, dW=dnorm2, eps=self.eps, p=p, seed=seed, offset=2 * step)
         dO = (da @ self.o).view(rows, self.heads, self.dim)
         q, k, v = self._split(qkv)
-        if self.ws is None:
-            self.ws = torch.empty(max(B.attention_backward_workspace_bytes(q, k, v, self.O, self.lse, cu), 1), dtype=torch.uint8, device=dout.device)
+        need = B.attention_backward_workspace_bytes(q, k, v, self.O, self.lse, cu)
+        if self.ws is None or self.ws.numel() < need:       # fewer sequences may take more
+            self.ws = torch.empty(need, dtype=torch.uint8, device=dout.device)
         if cu is not None:
             self.dqkv.zero_()
         B.attention_backward(q, k, v, self.O, self.lse, dO, *self._split(self.dqkv), cu=cu, ws=self.ws)

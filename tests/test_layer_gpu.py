@@ -68,6 +68,20 @@ def test_layer_gradients_against_autograd(dtype, tol, dropout):
         assert rel(grads[k], g64[k]) <= tol, k
 
 
+def test_layer_with_other_sequences_at_every_step():
+    # few sequences take a larger workspace of the attention's backward pass than many
+    rows = 1024
+    layer = DecoderLayer(rows, d=64, heads=8, kv_heads=1, ffn=96, seed=2)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    for n in (512, 1, 64):
+        cu = torch.arange(0, rows + 1, rows // n, dtype=torch.int32, device=DEV)
+        r, dout = torch.randn(rows, 64, generator=g, device=DEV), torch.randn(rows, 64, generator=g, device=DEV)
+        fresh = DecoderLayer(rows, d=64, heads=8, kv_heads=1, ffn=96, seed=2)
+        assert torch.equal(layer.forward(r, cu), fresh.forward(r, cu))
+        (dr, grads), (want, wants) = layer.backward(dout), fresh.backward(dout)
+        assert torch.equal(dr, want) and all(torch.equal(grads[k], wants[k]) for k in grads)
+
+
 def test_layer_gradients_through_statistics_roots_and_update():
     rows = 384
     layer = DecoderLayer(rows, d=256, heads=4, kv_heads=2, ffn=320, dropout=0.125)
