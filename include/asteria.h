@@ -513,16 +513,18 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  * int32[nseq + 1], ascending, within 0 .. total (read when the kernel runs; numbers outside are brought inside, but a descending
  * cu gives unspecified results); NULL: one sequence of `total` rows, nseq = 1.
  * Element (i, j, d) of Q lies at Q + i ldq + j hq + d, likewise the others: any strides and alignment; of written arrays rows
- * and heads may not overlap.  dtype fp32 or bf16; products on the bf16 matrix cores with fp32 sums, softmax in fp32.  bf16: P (and dS
+ * and heads may not overlap, nor one another or an array that is read.  dtype fp32 or bf16; products on the bf16 matrix cores with fp32 sums, softmax in fp32.  bf16: P (and dS
  * in the backward pass) is rounded to bf16 as an operand of the next product.  fp32: every operand is cut into three bf16 terms,
  * which keeps it to 2^-27; an infinite element has no such terms and counts as no number.  dim 1 .. 128.
+ * Sums over a row's keys are divided by the softmax's sum at the end, and may grow to 256 times the row's length times the
+ * largest |V|: beyond fp32's range they are infinite.
  * A row depends on no element of another sequence; within a sequence an element of K, V (or of dO, Q in the gradients of K and V) that is
  * no number or infinite may also reach up to 31 rows on the side that the mask hides from it.
  * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i, dP = dO V^T, dS = P (dP - D):
  *   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dK and dV summed over the heads that share them,
  * without atomics: every run gives the same bits.
  * Errors: NULL pointers, sizes <= 0, heads no multiple of kv_heads, bad dtype, scale not within 2^-100 .. 2^100, negative strides,
- * written arrays that overlap themselves, cu NULL with nseq > 1 -> INVALID_ARG; dim > 128, or (total / 128 + nseq) heads >= 2^24 -> UNSUPPORTED. */
+ * written arrays that overlap themselves or begin where another array does, cu NULL with nseq > 1 -> INVALID_ARG; dim > 128, or (total / 128 + nseq) heads >= 2^24 -> UNSUPPORTED. */
 typedef struct asteria_attn {
     const void *Q, *K, *V;
     void *O; /* written by asteria_attention, read by asteria_attention_backward */

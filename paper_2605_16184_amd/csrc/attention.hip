@@ -189,7 +189,7 @@ asteria_status validate(const asteria_attn *a, bool writes_o)
     if (a->heads % a->kv_heads || (!a->cu && a->nseq != 1) || !valid_dtype(a->dtype)) return ASTERIA_INVALID_ARG;
     if (!(a->scale >= 0x1p-100f && a->scale <= 0x1p100f)) return ASTERIA_INVALID_ARG;      // lse / scale and 8 / scale are numbers
     if (a->ldq < 0 || a->ldk < 0 || a->ldv < 0 || a->ldo < 0 || a->hq < 0 || a->hk < 0 || a->hv < 0 || a->ho < 0) return ASTERIA_INVALID_ARG;
-    if (writes_o && !apart(a->ldo, a->ho, a->total, a->heads, a->dim)) return ASTERIA_INVALID_ARG;
+    if (writes_o && (!apart(a->ldo, a->ho, a->total, a->heads, a->dim) || a->O == a->Q || a->O == a->K || a->O == a->V)) return ASTERIA_INVALID_ARG;
     if (a->dim > 128) return ASTERIA_UNSUPPORTED;
     if (((int64_t)a->total / 128 + 1 + a->nseq) * a->heads > MOST_BLOCKS) return ASTERIA_UNSUPPORTED;
     return ASTERIA_OK;
@@ -245,6 +245,9 @@ extern "C" asteria_status asteria_attention_backward(const asteria_attn *a, cons
     if (!a->lse || !g || !g->dO || !g->dQ || !g->dK || !g->dV || g->lddo < 0 || g->hdo < 0) return ASTERIA_INVALID_ARG;
     if (!apart(g->lddq, g->hdq, a->total, a->heads, a->dim) || !apart(g->lddk, g->hdk, a->total, a->kv_heads, a->dim) ||
         !apart(g->lddv, g->hdv, a->total, a->kv_heads, a->dim)) return ASTERIA_INVALID_ARG;
+    for (const void *out : {g->dQ, g->dK, g->dV})
+        if (out == a->Q || out == a->K || out == a->V || out == a->O || out == g->dO) return ASTERIA_INVALID_ARG;
+    if (g->dQ == g->dK || g->dQ == g->dV || g->dK == g->dV) return ASTERIA_INVALID_ARG;
     if (!ws || ws_bytes < asteria_attention_backward_workspace_bytes(a)) return ASTERIA_WORKSPACE_TOO_SMALL;
     if (reinterpret_cast<uintptr_t>(ws) & 255u) return ASTERIA_INVALID_ARG;   // workspace must be 256-byte aligned
     hipStream_t stream = reinterpret_cast<hipStream_t>(stream_);

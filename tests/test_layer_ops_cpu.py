@@ -126,6 +126,17 @@ def test_attention_backward_refuses_bad_gradients(bad):
     assert lib.asteria_attention_backward(_make(B._Attn, ATTN, {"lse": None}), _make(B._AttnGrad, GRAD, {}), WS, 1 << 20, None) == B.INVALID_ARG
 
 
+def test_attention_refuses_outputs_that_begin_where_another_array_does():
+    lib = ast.lib()
+    for name in ("Q", "K", "V"):
+        assert lib.asteria_attention(_make(B._Attn, ATTN, {"O": ATTN[name]}), None) == B.INVALID_ARG
+    read = [ATTN[name] for name in ("Q", "K", "V", "O")] + [GRAD["dO"]]
+    for out in ("dQ", "dK", "dV"):
+        for place in read + [GRAD[other] for other in ("dQ", "dK", "dV") if other != out]:
+            bad = _make(B._AttnGrad, GRAD, {out: place})
+            assert lib.asteria_attention_backward(_make(B._Attn, ATTN, {}), bad, WS, 1 << 20, None) == B.INVALID_ARG
+
+
 def test_attention_sizes_beyond_its_kernels_are_unsupported():
     lib = ast.lib()
     wide = dict(dim=129, ldq=129 * 4, hq=129, ldo=129 * 4, ho=129)
