@@ -32,10 +32,9 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) vo
     acc16 o[DP / 32];
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) o[t] = 0.0f;
-    // m, from which the exponents count, is the maximum of the first scores, and follows it only where a tile's sum of exponentials
-    // has passed 2^12: the tile is then computed again.  So no maximum is taken of the other tiles (3 % of the time), and sums and O are
-    // scaled rarely.
-    const float c = a.scale * LOG2E;
+    // the maximum m follows only where the scores have grown by more than 2^8 of it: sums and O are scaled rarely, and
+    // exp2 stays below 2^8
+    const float c = a.scale * LOG2E, slack = 8.0f / c;
     float m = -INFINITY, sum = 0.0f;
     const int last = min(tile.len, q0 + 32 * NA), nk = (last + BK - 1) / BK;
     AttStage<T, DP, BK, DIRECT> sk, sv;
@@ -74,64 +73,48 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) vo
         const typename M::Tile tk(lk + 32 * wb * NBLK * M::PITCH), tv(lv + 32 * wb * NBLK * M::PITCH);
         if (k0 > qw + 31) continue;                              // behind its rows
         acc16 s[NBLK];
-        auto scores = [&] {
 #pragma unroll
-            for (int b = 0; b < NBLK; ++b) s[b] = 0.0f;
+        for (int b = 0; b < NBLK; ++b) s[b] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) {
-                if (att_empty<T, DP>(d, a.dim)) break;
+        for (int d = 0; d < DP / 16; ++d) {
+            if (att_empty<T, DP>(d, a.dim)) break;
 #pragma unroll
-                for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s[b]);
-            }
-            if (k0 + 32 * NBLK - 1 > qw) {
-#pragma unroll
-                for (int b = 0; b < NBLK; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) if (k0 + 32 * b + acc_row(i, h) > qi) s[b][i] = -INFINITY;
-            }
-        };
-        auto rise = [&] {
-            float top = s[0][0];
+            for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s[b]);
+        }
+        if (k0 + 32 * NBLK - 1 > qw) {
 #pragma unroll
             for (int b = 0; b < NBLK; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-            const float to = fmaxf(m, join_halves<true>(top)), f = to == m ? 1.0f : __builtin_amdgcn_exp2f((m - to) * c);
+                for (int i = 0; i < 16; ++i) if (k0 + 32 * b + acc_row(i, h) > qi) s[b][i] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < NBLK; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = join_halves<true>(top);
+        if (__any(top > m + slack)) {
+            const float to = fmaxf(m, top), f = to == m ? 1.0f : __builtin_amdgcn_exp2f((m - to) * c);
             m = to;
             sum *= f;
 #pragma unroll
             for (int t = 0; t < DP / 32; ++t) o[t] *= f;
-        };
-        auto exponentials = [&] {
-            const float mc = m == -INFINITY ? 0.0f : m * c;
-            float part[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int b = 0; b < NBLK; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc));
-                    part[i & 1] += s[b][i];                      // before the rounding to an operand: lse is fp32
-                }
-            return part[0] + part[1];
-        };
-        scores();
-        const bool none = __any(m == -INFINITY);                 // so far no score to go by
-        if (none) rise();
-        float part = exponentials();
-        if (!none && __any(!(part <= 4096.0f))) {
-            scores();
-            rise();
-            part = exponentials();
         }
-        sum += part;
+        const float mc = m == -INFINITY ? 0.0f : m * c;
 #pragma unroll
-        for (int b = 0; b < NBLK; ++b)
+        for (int b = 0; b < NBLK; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc));
+                sum += s[b][i];                                  // before the rounding to an operand: lse is fp32
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const typename M::held p = M::pack(s[b], 8 * k);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tv, 32 * b + 16 * k, 32 * t), p, o[t]);
             }
+        }
     }
     sum = join_halves<false>(sum);
     if constexpr (NB > 1) {
