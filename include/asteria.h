@@ -516,8 +516,8 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  * and heads may not overlap, nor one another or an array that is read.  dtype fp32 or bf16; products on the bf16 matrix cores with fp32 sums, softmax in fp32.  bf16: P (and dS
  * in the backward pass) is rounded to bf16 as an operand of the next product.  fp32: every operand is cut into three bf16 terms,
  * which keeps it to 2^-27; an infinite element has no such terms and counts as no number.  dim 1 .. 128.
- * Sums over a row's keys are divided by the softmax's sum at the end, and may grow to 256 times the row's length times the
- * largest |V|: beyond fp32's range they are infinite.
+ * Sums over a row's keys are divided by the softmax's sum at the end, and may grow to 2^41 times the largest |V|: beyond fp32's
+ * range they are infinite.
  * A row depends on no element of another sequence; within a sequence an element of K, V (or of dO, Q in the gradients of K and V) that is
  * no number or infinite may also reach up to 31 rows on the side that the mask hides from it.
  * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i, dP = dO V^T, dS = P (dP - D):

@@ -320,9 +320,10 @@ template <int DP, int BK> struct AttStage<bf16_elem, DP, BK, true> {
     __device__ __forceinline__ void init(const AttArray &a, int row0, int head, int first, int rows, int dim_)
     {
         ld = (int)a.ld * 2;
-        base = reinterpret_cast<uint64_t>(att_at<const bf16_elem>(a, row0 + first, head));
+        const uint64_t at = reinterpret_cast<uint64_t>(att_at<const bf16_elem>(a, row0 + first, head));
+        base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
         dim = dim_;
-        left = (rows - first - 1) * ld + dim * 2;
+        left = __builtin_amdgcn_readfirstlane((rows - first - 1) * ld + dim * 2);
     }
     // the next BK rows to `stage`; the rows after them are next.  SPARE: a lane's place is made anew for every tile - kept, it is a
     // register that the gradients of K and V do not have.

@@ -13,6 +13,13 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct FwdShape {
     static_assert(LDS >= (NB / 2) * NA * DP * 32 * sizeof(float) && LDS >= NB * NA * 64 * sizeof(float), "room for the sums");
 };
 
+// A workgroup takes 128 rows of a head (NA = 4 wavefronts of 32), or fewer rows with NB wavefronts each, and passes over their keys and values, tile
+// by tile through two stages of LDS: the next tile is on its way while this one is multiplied, with one barrier a tile.
+// Bound by the vector units more than by the matrix cores: 32 x 32 scores and their products with a head of 64 are 256 cycles of the
+// latter, their exponentials, sums and roundings 1.7 times as many of the former, and two wavefronts a SIMD overlap them in part.
+// Measured: 8192 rows, 32 heads of 64 on 4 (275 GFLOP of causal products): 294 us, 935 TFLOP/s, matrix cores busy 41 % and vector units
+// 71 % of the time at 1.8 - 1.95 GHz (the power limit), no LDS conflicts; 4 x 2048 rows 85 us, 8123 packed rows, 16 heads of 128: 81 us.
+// fp32: 8192 rows, 16 heads of 64: 209 us.
 template <typename T, int DP, int NA, int NB, bool DIRECT>
 __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attention_kernel(AttArgs a)
 {
@@ -30,91 +37,126 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) vo
     typename M::held q[DP / 16];
     load_frags<T, DP>(a.Q, tile.start + qi, head, valid, a.dim, q);
     acc16 o[DP / 32];
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t) o[t] = 0.0f;
-    // the maximum m follows only where the scores have grown by more than 2^8 of it: sums and O are scaled rarely, and
-    // exp2 stays below 2^8
-    const float c = a.scale * LOG2E, slack = 8.0f / c;
-    float m = -INFINITY, sum = 0.0f;
+    // Exponents count from m.  bf16: m is the maximum of the first tile's scores and rises only where the sum has passed 2^20, by that
+    // sum's logarithm; no maximum is taken of the other tiles.  Should the scores of one tile lift the sum beyond 2^40, the
+    // workgroup begins again, in a pass (SAFE) that takes every tile's maximum before its exponentials and follows it by steps of 2^8
+    // or more, and costs the time of both: 303 us for 8192 rows where the first kind takes 289.  fp32, whose six products a tile leave the vector units time, has
+    // only the second kind (2013 rows, 8 heads of 80: 67 us, 69 with the first).
+    const float c = a.scale * LOG2E;
+    float m, sum;
     const int last = min(tile.len, q0 + 32 * NA), nk = (last + BK - 1) / BK;
     AttStage<T, DP, BK, DIRECT> sk, sv;
-    if constexpr (DIRECT) {
-        sk.init(a.K, tile.start, kvh, 0, last, a.dim);
-        sv.init(a.V, tile.start, kvh, 0, last, a.dim);
-        sk.template issue<false>(lk);
-        sv.template issue<false>(lv);
-    } else {
-        sk.load(a.K, tile.start, kvh, last, a.dim);
-        sv.load(a.V, tile.start, kvh, last, a.dim);
-    }
-    arrived(q);
-    for (int kt = 0; kt < nk; ++kt) {
-        const int k0 = kt * BK + wb * 32 * NBLK, next = (kt + 1) * BK;   // k0: of this wavefront's keys
+    auto pass = [&](auto safe_) -> bool {
+        constexpr bool SAFE = decltype(safe_)::value;
+        bool fails = false;
+        m = -INFINITY;
+        sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) o[t] = 0.0f;
+        lk = reinterpret_cast<T *>(lds);
+        lv = lk + TILE;
         if constexpr (DIRECT) {
-            lk = reinterpret_cast<T *>(lds) + (kt & 1) * 2 * TILE;
-            lv = lk + TILE;
-            wait_lds_loads<0>();
-            __syncthreads();
-            if (kt + 1 < nk) {
-                T *to = reinterpret_cast<T *>(lds) + (~kt & 1) * 2 * TILE;
-                sk.template issue<false>(to);
-                sv.template issue<false>(to + TILE);
-            }
+            sk.init(a.K, tile.start, kvh, 0, last, a.dim);
+            sv.init(a.V, tile.start, kvh, 0, last, a.dim);
+            sk.template issue<false>(lk);
+            sv.template issue<false>(lv);
         } else {
-            __syncthreads();
-            sk.store(lk);
-            sv.store(lv);
-            __syncthreads();
-            if (kt + 1 < nk) {
-                sk.load(a.K, tile.start + next, kvh, last - next, a.dim);
-                sv.load(a.V, tile.start + next, kvh, last - next, a.dim);
+            sk.load(a.K, tile.start, kvh, last, a.dim);
+            sv.load(a.V, tile.start, kvh, last, a.dim);
+        }
+        arrived(q);
+        for (int kt = 0; kt < nk; ++kt) {
+            const int k0 = kt * BK + wb * 32 * NBLK, next = (kt + 1) * BK;   // k0: of this wavefront's keys
+            if constexpr (DIRECT) {
+                lk = reinterpret_cast<T *>(lds) + (kt & 1) * 2 * TILE;
+                lv = lk + TILE;
+                wait_lds_loads<0>();
+                __syncthreads();
+                if (kt + 1 < nk) {
+                    T *to = reinterpret_cast<T *>(lds) + (~kt & 1) * 2 * TILE;
+                    sk.template issue<false>(to);
+                    sv.template issue<false>(to + TILE);
+                }
+            } else {
+                __syncthreads();
+                sk.store(lk);
+                sv.store(lv);
+                __syncthreads();
+                if (kt + 1 < nk) {
+                    sk.load(a.K, tile.start + next, kvh, last - next, a.dim);
+                    sv.load(a.V, tile.start + next, kvh, last - next, a.dim);
+                }
+            }
+            const typename M::Tile tk(lk + 32 * wb * NBLK * M::PITCH), tv(lv + 32 * wb * NBLK * M::PITCH);
+            if (k0 > qw + 31) continue;                              // behind its rows
+            acc16 s[NBLK];
+#pragma unroll
+            for (int b = 0; b < NBLK; ++b) s[b] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                if (att_empty<T, DP>(d, a.dim)) break;
+#pragma unroll
+                for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s[b]);
+            }
+            if (k0 + 32 * NBLK - 1 > qw) {
+#pragma unroll
+                for (int b = 0; b < NBLK; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) if (k0 + 32 * b + acc_row(i, h) > qi) s[b][i] = -INFINITY;
+            }
+            if (SAFE || kt == 0) {
+                float top = s[0][0];
+#pragma unroll
+                for (int b = 0; b < NBLK; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+                top = join_halves<true>(top) * c;
+                if (!SAFE) {
+                    m = top;
+                    fails = top == -INFINITY && k0 <= qi;            // no score to count from
+                } else if (__any(top > m + 8.0f)) {
+                    const float to = fmaxf(m, top), f = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+                    m = to;
+                    sum *= f;
+#pragma unroll
+                    for (int t = 0; t < DP / 32; ++t) o[t] *= f;
+                }
+            }
+            const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int b = 0; b < NBLK; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -from));
+                    sum += s[b][i];                                  // before the rounding to an operand: lse is fp32
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const typename M::held p = M::pack(s[b], 8 * k);
+#pragma unroll
+                    for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tv, 32 * b + 16 * k, 32 * t), p, o[t]);
+                }
+            }
+            if (!SAFE && __any(sum > 0x1p20f)) {
+                const float all = join_halves<true>(sum), to = all > 0x1p20f ? m + __builtin_amdgcn_logf(all) : m;
+                fails |= !(all <= 0x1p40f);
+                const float f = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                sum *= f;
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) o[t] *= f;
             }
         }
-        const typename M::Tile tk(lk + 32 * wb * NBLK * M::PITCH), tv(lv + 32 * wb * NBLK * M::PITCH);
-        if (k0 > qw + 31) continue;                              // behind its rows
-        acc16 s[NBLK];
-#pragma unroll
-        for (int b = 0; b < NBLK; ++b) s[b] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DP / 16; ++d) {
-            if (att_empty<T, DP>(d, a.dim)) break;
-#pragma unroll
-            for (int b = 0; b < NBLK; ++b) s[b] = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s[b]);
-        }
-        if (k0 + 32 * NBLK - 1 > qw) {
-#pragma unroll
-            for (int b = 0; b < NBLK; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) if (k0 + 32 * b + acc_row(i, h) > qi) s[b][i] = -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int b = 0; b < NBLK; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = join_halves<true>(top);
-        if (__any(top > m + slack)) {
-            const float to = fmaxf(m, top), f = to == m ? 1.0f : __builtin_amdgcn_exp2f((m - to) * c);
-            m = to;
-            sum *= f;
-#pragma unroll
-            for (int t = 0; t < DP / 32; ++t) o[t] *= f;
-        }
-        const float mc = m == -INFINITY ? 0.0f : m * c;
-#pragma unroll
-        for (int b = 0; b < NBLK; ++b) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc));
-                sum += s[b][i];                                  // before the rounding to an operand: lse is fp32
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const typename M::held p = M::pack(s[b], 8 * k);
-#pragma unroll
-                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tv, 32 * b + 16 * k, 32 * t), p, o[t]);
-            }
-        }
+        return fails || !(sum <= 0x1p40f);
+    };
+    if constexpr (sizeof(T) == 4) {
+        pass(std::true_type());
+    } else {
+        __shared__ int failed;
+        if (threadIdx.x == 0) failed = 0;            // the pass has barriers before its end
+        if (pass(std::false_type())) failed = 1;
+        __syncthreads();
+        if (__builtin_amdgcn_readfirstlane(failed)) pass(std::true_type());
     }
     sum = join_halves<false>(sum);
     if constexpr (NB > 1) {
@@ -129,9 +171,9 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) vo
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
             const float mk = ms[(k * NA + wa) * 32 + (l & 31)];
-            all += ms[(NA * NB + k * NA + wa) * 32 + (l & 31)] * (mk == top ? 1.0f : __builtin_amdgcn_exp2f((mk - top) * c));
+            all += ms[(NA * NB + k * NA + wa) * 32 + (l & 31)] * (mk == top ? 1.0f : __builtin_amdgcn_exp2f(mk - top));
         }
-        const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f((m - top) * c);
+        const float f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) o[t] *= f;
         m = top;
@@ -141,7 +183,7 @@ __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) vo
     }
     if (!valid) return;
     store_row<T, DP>(att_at<T>(a.O, tile.start + qi, head), a.dim, o, 1.0f / sum);
-    if (a.lse && h == 0) a.lse[(size_t)head * a.total + tile.start + qi] = (m * c + __builtin_amdgcn_logf(sum)) * LN2;
+    if (a.lse && h == 0) a.lse[(size_t)head * a.total + tile.start + qi] = (m + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(const AttArgs &a, hipStream_t stream)

@@ -504,6 +504,28 @@ def test_attention_scores_that_rise_and_fall(heads, dtype):
         _inside(lse[j, 210:], torch.logsumexp(z, 1), torch.full((n - 210,), 504 * 8 * F, dtype=torch.float64, device=DEV), "lse")
 
 
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("heads", [1, 192])
+@pytest.mark.parametrize("step", [4.0, 15.0, 20.0, 45.0, -20.0])
+def test_attention_scores_in_steps(step, heads, dtype):
+    # every 90 keys the scores are a step higher: sums grow by 2^6, 2^21, 2^29, 2^65 at a time
+    n = 500
+    Q, K, V = torch.zeros(n, heads, 64, device=DEV), torch.zeros(n, 1, 64, device=DEV), _randn(n, 1, 64, seed=3)
+    Q[:, :, 0] = 1.0
+    K[:, 0, 0] = step * (torch.arange(n, device=DEV) // 90)
+    Q, K, V = Q.to(dtype), K.to(dtype), V.to(dtype)
+    O, lse = torch.empty_like(Q), torch.empty(heads, n, device=DEV)
+    ast.attention(Q, K, V, O, lse=lse, scale=1.0)
+    top = abs(step) * 5 + 10
+    z = torch.where(torch.ones(n, n, device=DEV).tril().bool(), K[:, 0, 0].double().expand(n, n), -math.inf)
+    P = torch.softmax(z, 1)
+    # roundings of the result, of P, of the exponents and of the sums
+    tol = (U[dtype] * 1.01 + (U[bf16] * 1.01 if dtype == bf16 else 0.0) + 2 * top * 4 * F + 1000 * F) * (P @ V[:, 0].double().abs())
+    for j in (0, heads - 1):
+        _inside(O[:, j], P @ V[:, 0].double(), tol, "O")
+        _inside(lse[j], torch.logsumexp(z, 1), torch.full((n,), top * 8 * F, dtype=torch.float64, device=DEV), "lse")
+
+
 def test_attention_gradient_against_differences():
     # of the forward pass in 64 bits, along one random direction of all three inputs
     Q, K, V, dO = (_randn(130, h, 40, seed=i) for i, h in enumerate((4, 2, 2, 4)))
