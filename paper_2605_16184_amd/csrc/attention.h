@@ -96,7 +96,7 @@ template <int DP> struct Op<bf16_elem, DP> {
 // fp32: every operand as three bf16 terms, x = hi + mid + lo with the rest below 2^-27 of x, and of the nine products the six above
 // 2^-26: six instructions of 32 cycles where the fp32 matrix cores take eight of 64 for the same 16 places, and the sums are fp32.  A
 // tile is cut once, on its way to LDS, where the terms of a row lie one behind the other (cut by every wavefront that reads it, the
-// vector units were the bound: 580 us instead of 475 us a forward pass of 8192 rows, 16 heads of 128).  An infinite element has no such terms:
+// vector units were the bound: 580 us instead of 475 us a forward pass of 4 x 2048 rows, 16 heads of 128).  An infinite element has no such terms:
 // it counts as no number.
 template <int DP> struct Op<float, DP> {
     typedef float T;
@@ -483,7 +483,7 @@ template <typename T> constexpr int att_shared = sizeof(T) == 4 ? 2 : 4;
 template <typename T, int DP> __device__ __forceinline__ bool att_empty(int d, int dim) { return sizeof(T) == 4 && DP == 96 && d == 5 && dim <= 80; }
 
 // LDS to ask for.  fp32 workgroups that would all run at once, two a CU, are given so much that one has the CU: the longest then
-// do not share one while others stand idle (8192 rows, 8 heads of 64: forward 213 -> 176 us).
+// do not share one while others stand idle (4 x 2048 rows, 8 heads of 64: forward 213 -> 176 us).
 template <typename T, int NB> constexpr size_t att_lds(size_t need, int64_t blocks)
 {
     return sizeof(T) == 4 && NB == 1 && blocks < 1024 && need < 84 * 1024 ? 84 * 1024 : need;

@@ -16,10 +16,11 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct FwdShape {
 // A workgroup takes 128 rows of a head (NA = 4 wavefronts of 32), or fewer rows with NB wavefronts each, and passes over their keys and values, tile
 // by tile through two stages of LDS: the next tile is on its way while this one is multiplied, with one barrier a tile.
 // Bound by the vector units more than by the matrix cores: 32 x 32 scores and their products with a head of 64 are 256 cycles of the
-// latter, their exponentials, sums and roundings 1.7 times as many of the former, and two wavefronts a SIMD overlap them in part.
-// Measured: 8192 rows, 32 heads of 64 on 4 (275 GFLOP of causal products): 294 us, 935 TFLOP/s, matrix cores busy 41 % and vector units
-// 71 % of the time at 1.8 - 1.95 GHz (the power limit), no LDS conflicts; 4 x 2048 rows 85 us, 8123 packed rows, 16 heads of 128: 81 us.
-// fp32: 8192 rows, 16 heads of 64: 209 us.
+// latter, their exponentials, sums and roundings 1.5 times as many of the former, and up to four wavefronts a SIMD overlap them.
+// Measured: 8192 rows, 32 heads of 64 on 4 (275 GFLOP of causal products): 282 - 290 us, 950 - 975 TFLOP/s, matrix cores busy 50 % and
+// vector units 72 % of the time at 1.8 - 1.95 GHz (the power limit), no LDS conflicts; 4 x 2048 rows 85 us, 8123 packed rows, 16 heads
+// of 128: 81 us.
+// fp32: 4 x 2048 rows, 16 heads of 64: 209 us.
 template <typename T, int DP, int NA, int NB, bool DIRECT>
 __global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attention_kernel(AttArgs a)
 {

