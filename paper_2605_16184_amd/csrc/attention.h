@@ -482,11 +482,13 @@ template <typename T> constexpr int att_shared = sizeof(T) == 4 ? 2 : 4;
 // The last 16 columns of fp32 heads of 65 to 80, which are padding only, are left out of the products over dim (a head of 80: 3 %).
 template <typename T, int DP> __device__ __forceinline__ bool att_empty(int d, int dim) { return sizeof(T) == 4 && DP == 96 && d == 5 && dim <= 80; }
 
-// LDS to ask for.  fp32 workgroups that would all run at once, two a CU, are given so much that one has the CU: the longest then
-// do not share one while others stand idle (4 x 2048 rows, 8 heads of 64: forward 213 -> 176 us).
-template <typename T, int NB> constexpr size_t att_lds(size_t need, int64_t blocks)
+// LDS to ask for, in kernels of which PER_CU workgroups fit a CU.  Workgroups that would all run at once are given so much that fewer
+// share a CU: the longest then do not share one while others stand idle.  fp32, below 1024 workgroups: one (4 x 2048 rows, 8 heads of
+// 64: forward 213 -> 176 us).  bf16, three a CU, below 768: two (backward, heads of 64: 740 workgroups 130 -> 123 us; at 888 146 -> 148).
+template <typename T, int NB, int PER_CU> constexpr size_t att_lds(size_t need, int64_t blocks)
 {
-    return sizeof(T) == 4 && NB == 1 && blocks < 1024 && need < 84 * 1024 ? 84 * 1024 : need;
+    const size_t more = sizeof(T) == 4 ? 84 * 1024 : 56 * 1024;
+    return NB == 1 && (sizeof(T) == 4 || PER_CU == 3) && blocks < (sizeof(T) == 4 ? 1024 : 768) && need < more ? more : need;
 }
 
 // Kernels for dims padded to 64, 96 or 128.

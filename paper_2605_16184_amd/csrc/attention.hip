@@ -10,6 +10,7 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct FwdShape {
     static constexpr int BK = 32 * (NB > 1 ? NB : Op<T, DP>::BLOCKS);
     static constexpr int TILE = BK * Op<T, DP>::PITCH;
     static constexpr size_t LDS = (DIRECT ? 4 : 2) * (size_t)TILE * sizeof(T);
+    static constexpr int PER_CU = sizeof(T) == 2 || DP == 64 ? 2 : 1;       // workgroups a CU, or more
     static_assert(LDS >= (NB / 2) * NA * DP * 32 * sizeof(float) && LDS >= NB * NA * 64 * sizeof(float), "room for the sums");
 };
 
@@ -22,7 +23,7 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct FwdShape {
 // of 128: 81 us.
 // fp32: 4 x 2048 rows, 16 heads of 64: 209 us.
 template <typename T, int DP, int NA, int NB, bool DIRECT>
-__global__ __launch_bounds__(ATT_THREADS, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attention_kernel(AttArgs a)
+__global__ __launch_bounds__(ATT_THREADS, (FwdShape<T, DP, NA, NB, DIRECT>::PER_CU)) void attention_kernel(AttArgs a)
 {
     typedef Op<T, DP> M;
     constexpr int BK = FwdShape<T, DP, NA, NB, DIRECT>::BK, NBLK = BK / 32 / NB;
@@ -191,8 +192,9 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(con
 {
     static bool configured[MAX_DEVICES] = {};
     const int64_t blocks = att_tiles(a, 32 * NA) * a.heads;
-    constexpr size_t MOST = att_lds<T, NB>(FwdShape<T, DP, NA, NB, DIRECT>::LDS, 0);
-    const size_t bytes = att_lds<T, NB>(FwdShape<T, DP, NA, NB, DIRECT>::LDS, blocks);
+    typedef FwdShape<T, DP, NA, NB, DIRECT> Shape;
+    constexpr size_t MOST = att_lds<T, NB, Shape::PER_CU>(Shape::LDS, 0);
+    const size_t bytes = att_lds<T, NB, Shape::PER_CU>(Shape::LDS, blocks);
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(attention_kernel<T, DP, NA, NB, DIRECT>), MOST, configured); e != hipSuccess) return e;
     hipLaunchKernelGGL((attention_kernel<T, DP, NA, NB, DIRECT>), dim3((unsigned)blocks), dim3(ATT_THREADS), bytes, stream, a);
     return hipGetLastError();
