@@ -1,9 +1,10 @@
 // Gradients of K and V (attention.h): a wavefront holds the keys and values of 32 rows in registers and passes over the
 // rows that see them, in all the heads that share them.
 //
-// Four products a tile; 128 accumulators and the held keys and values leave room for two wavefronts a SIMD (1.65 resident on average), which
-// is what bounds it: matrix cores busy 36 %, vector units 37 %.  Measured: 4 x 2048 rows, 32 heads of 64 on 4: 169 us, 810 TFLOP/s of
-// causal products; 8123 packed rows, 16 heads of 128 on 4: 156 us.  With 64 keys a wavefront the backward pass takes 365 instead of 325 us.
+// Four products a tile; accumulators and the held keys and values leave room for three wavefronts a SIMD (heads of up to 64; two with
+// longer ones), of which 1.8 (1.6) are resident on average, and that bounds it: matrix cores and vector units are busy 35 % of the time.
+// Measured: 4 x 2048 rows, 32 heads of 64 on 4: 146 us, 940 TFLOP/s of causal products; 8123 packed rows, 16 heads of 128 on 4: 153 - 160 us.
+// With 64 keys a wavefront the backward pass of the former took 365 instead of 325 us.
 //
 // Where the heads that share keys are many and the tiles are few, several workgroups take a part of these heads each, leave
 // their sums in fp32 in the workspace, and a second kernel adds them up: without atomics, in one order.
@@ -217,7 +218,8 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(con
 
 }  // namespace
 
-// The sums of a part of the heads are written and read once more in fp32, so as few parts as give the card four workgroups a CU.
+// The sums of a part of the heads are written and read once more in fp32, so as few parts as give the card four workgroups a CU:
+// the backward pass of 4 x 2048 rows, 32 heads on 4, 284 us, 302 with 1536 and 343 with 512 workgroups as the mark.
 int asteria::attention_splits(const AttArgs &a)
 {
     const int64_t tiles = att_tiles(a, 128) * (a.heads / a.group);
