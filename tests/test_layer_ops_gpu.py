@@ -507,10 +507,11 @@ def test_attention_scores_that_rise_and_fall(heads, dtype):
 @pytest.mark.parametrize("dtype", [bf16, f32])
 @pytest.mark.parametrize("heads", [1, 192])
 @pytest.mark.parametrize("step", [4.0, 15.0, 20.0, 45.0, -20.0])
-def test_attention_scores_in_steps(step, heads, dtype):
+@pytest.mark.parametrize("dim", [64, 33, 120])
+def test_attention_scores_in_steps(dim, step, heads, dtype):
     # every 90 keys the scores are a step higher: sums grow by 2^6, 2^21, 2^29, 2^65 at a time
     n = 500
-    Q, K, V = torch.zeros(n, heads, 64, device=DEV), torch.zeros(n, 1, 64, device=DEV), _randn(n, 1, 64, seed=3)
+    Q, K, V = torch.zeros(n, heads, dim, device=DEV), torch.zeros(n, 1, dim, device=DEV), _randn(n, 1, dim, seed=3)
     Q[:, :, 0] = 1.0
     K[:, 0, 0] = step * (torch.arange(n, device=DEV) // 90)
     Q, K, V = Q.to(dtype), K.to(dtype), V.to(dtype)
