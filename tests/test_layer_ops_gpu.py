@@ -527,6 +527,34 @@ def test_attention_scores_in_steps(dim, step, heads, dtype):
         _inside(lse[j], torch.logsumexp(z, 1), torch.full((n,), top * 8 * F, dtype=torch.float64, device=DEV), "lse")
 
 
+@pytest.mark.parametrize("dim", [64, 50, 128])
+@pytest.mark.parametrize("n,heads", [(3, 1), (20, 1), (20, 400), (64, 1), (64, 400), (300, 1), (300, 200)])
+def test_attention_gradients_without_the_rounding_of_o(n, heads, dim):
+    # values around 64, where O is stored in steps of 1/2: D from it would be off by a tenth of dP - D.  The gradient of K is free of
+    # that at every length, that of Q where a row's keys lie in one tile
+    Q, K, dO = _randn(n, heads, dim, dtype=bf16, seed=1), _randn(n, 1, dim, dtype=bf16, seed=2), _randn(n, heads, dim, dtype=bf16, seed=4)
+    V = (64 + _randn(n, 1, dim, seed=3)).to(bf16)
+    O, lse, dQ, dK, dV = torch.empty_like(Q), torch.empty(heads, n, device=DEV), torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)
+    ast.attention(Q, K, V, O, lse=lse)
+    ast.attention_backward(Q, K, V, O, lse, dO, dQ, dK, dV)
+    some = sorted({0, heads - 1})
+    q, k, v, g, scale = Q.double(), K[:, 0].double().contiguous(), V[:, 0].double().contiguous(), dO.double(), dim ** -0.5
+    wantK = torch.zeros_like(k)
+    # independent roundings of dS and of the result, each within half a step; sums of dim products of size 64, in fp32, against differences of size 1
+    bound = math.sqrt(2) * U[bf16] + 64 * dim * F
+    for j in range(heads):
+        qj, gj = q[:, j].contiguous(), g[:, j].contiguous()
+        z = torch.where(torch.ones(n, n, device=DEV).tril().bool(), scale * torch.mm(qj, k.T.contiguous()), -math.inf)
+        P = torch.softmax(z, 1)
+        dP = torch.mm(gj, v.T.contiguous())
+        dS = P * (dP - (P * dP).sum(1, keepdim=True))
+        wantK += scale * torch.mm(dS.T.contiguous(), qj)
+        if n <= 64 and j in some:
+            want = scale * torch.mm(dS, k)
+            assert float(torch.linalg.norm(dQ[:, j].double() - want) / torch.linalg.norm(want)) <= bound
+    assert float(torch.linalg.norm(dK[:, 0].double() - wantK) / torch.linalg.norm(wantK)) <= bound
+
+
 def test_attention_gradient_against_differences():
     # of the forward pass in 64 bits, along one random direction of all three inputs
     Q, K, V, dO = (_randn(130, h, 40, seed=i) for i, h in enumerate((4, 2, 2, 4)))
