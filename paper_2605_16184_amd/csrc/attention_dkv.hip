@@ -3,7 +3,7 @@
 //
 // Four products a tile; accumulators and the held keys and values leave room for three wavefronts a SIMD (heads of up to 64; two with
 // longer ones), of which 1.8 (1.6) are resident on average, and that bounds it: matrix cores and vector units are busy 35 % of the time.
-// Measured: 4 x 2048 rows, 32 heads of 64 on 4: 146 us, 940 TFLOP/s of causal products; 8123 packed rows, 16 heads of 128 on 4: 153 - 160 us.
+// Measured: 4 x 2048 rows, 32 heads of 64 on 4: 145 us, 940 TFLOP/s of causal products; 8123 packed rows, 16 heads of 128 on 4: 157 us.
 // With 64 keys a wavefront the backward pass of the former took 365 instead of 325 us.
 //
 // Where the heads that share keys are many and the tiles are few, several workgroups take a part of these heads each, leave

@@ -3,8 +3,8 @@
 // The tiles and stages of the forward pass, with three products a tile instead of two.  A kernel of its own, beside that of K and V,
 // which computes scores and dP once more (7 products instead of 5): one kernel for all would add dQ up over workgroups, by
 // atomics whose order changes the result or through partial sums in memory (570 MB for 4 x 2048 rows, 32 heads of 64).  Measured: those rows
-// 122 us, 850 TFLOP/s of causal products, matrix cores busy 40 % and vector units 47 %, 2.4 wavefronts a SIMD; 8123 packed rows, 16 heads
-// of 128: 119 us.
+// 129 us, 800 TFLOP/s of causal products, matrix cores busy 40 % and vector units 48 %, 2.4 wavefronts a SIMD; 8123 packed rows, 16 heads
+// of 128: 125 us.
 #include "attention.h"
 #include "gemm.h"
 
