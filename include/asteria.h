@@ -520,8 +520,8 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  * range they are infinite.
  * A row depends on no element of another sequence; within a sequence an element of K, V (or of dO, Q in the gradients of K and V) that is
  * no number or infinite may also reach up to 31 rows on the side that the mask hides from it.
- * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i (bf16: without O's rounding in dK, and in dQ for
- * the first rows of a sequence), dP = dO V^T, dS = P (dP - D):
+ * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i (bf16: without O's rounding, as the sum of a row of
+ * dS gives it), dP = dO V^T, dS = P (dP - D):
  *   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dK and dV summed over the heads that share them,
  * without atomics: every run gives the same bits.
  * Errors: NULL pointers, sizes <= 0, heads no multiple of kv_heads, bad dtype, scale not within 2^-100 .. 2^100, negative strides,

@@ -7,7 +7,7 @@
 // operand of the next product lane l holds column l % 32 and eight of 16 places of the contraction, whose order is free as long
 // as the first operand follows it.  So
 //   forward        S^T = K Q^T,  O^T += V^T P^T             a lane holds one query; V^T read from LDS with transposing loads
-//   gradient of Q  S^T = K Q^T,  dP^T = V dO^T,  dQ^T += K^T dS^T
+//   gradient of Q  S^T = K Q^T,  dP^T = V dO^T,  dQ^T += K^T dS^T  (bf16: K^T P^T, too)
 //   of K and V     S = Q K^T,  dP = dO V^T,  dV^T += dO^T P,  dK^T += Q^T dS     a lane holds one key
 // All products run on v_mfma_f32_32x32x16_bf16: bf16 operands as they are, fp32 operands in three terms.
 #pragma once

@@ -1,10 +1,9 @@
 // Gradient of Q (attention.h); and for the gradients of K and V, at which their sums begin: -lse / scale and -D, D = rowsum(dO o O).
 //
-// The tiles and stages of the forward pass, with three products a tile instead of two.  A kernel of its own, beside that of K and V,
-// which computes scores and dP once more (7 products instead of 5): one kernel for all would add dQ up over workgroups, by
-// atomics whose order changes the result or through partial sums in memory (570 MB for 4 x 2048 rows, 32 heads of 64).  Measured: those rows
-// 129 us, 800 TFLOP/s of causal products, matrix cores busy 40 % and vector units 48 %, 2.4 wavefronts a SIMD; 8123 packed rows, 16 heads
-// of 128: 125 us.
+// The tiles and stages of the forward pass, with three products a tile instead of two (four in bf16).  A kernel of its own, beside that
+// of K and V, which computes scores and dP once more: one kernel for all would add dQ up over workgroups, by atomics whose order
+// changes the result or through partial sums in memory (570 MB for 4 x 2048 rows, 32 heads of 64).  Measured: those rows 148 us, 930
+// TFLOP/s of causal products; 8123 packed rows, 16 heads of 128: 148 us.
 #include "attention.h"
 #include "gemm.h"
 
@@ -13,10 +12,17 @@ using namespace asteria;
 namespace {
 
 template <typename T, int DP, int NA, int NB, bool DIRECT> struct DqShape {
-    static constexpr int BK = 32 * (NB > 1 ? NB : Op<T, DP>::BLOCKS);
+    static constexpr bool B16 = sizeof(T) == 2, LONE = B16 && NB > 1 && !DIRECT && DP > 64;
+    // 32 keys a stage where registers are short: two blocks side by side take 16 more of them.  4 x 2048 rows, 16 heads of 128, backward:
+    // 322 us so, 353 with 64 keys; heads of 65 in rows of no whole pieces: 497 and 507 us.
+    static constexpr int BK = 32 * (NB > 1 ? NB : B16 && (DP == 128 || (DP == 96 && !DIRECT)) ? 1 : Op<T, DP>::BLOCKS);
     static constexpr int TILE = BK * Op<T, DP>::PITCH;
-    static constexpr size_t LDS = (DIRECT ? 4 : 2) * (size_t)TILE * sizeof(T);
-    static constexpr int PER_CU = sizeof(T) == 2 && DP == 64 && DIRECT ? 3 : sizeof(T) == 2 || DP == 64 ? 2 : 1;      // workgroups a CU
+    // Pieces of dO that stay in LDS, so that two accumulators of dim x 32 fit the registers of PER_CU workgroups.
+    static constexpr int HELD = !B16 || LONE ? 0 : DP == 64 ? (DIRECT && NB == 1 ? 2 : 0) : DP == 96 ? 3 : DIRECT ? 5 : 7;
+    static constexpr size_t STAGED = (DIRECT ? 4 : 2) * (size_t)TILE * sizeof(T), LDS = STAGED + HELD * NA * NB * 64 * 16;
+    // Workgroups a CU: three with heads of up to 64 in bf16 (backward pass of 4 x 2048 rows, 32 heads: 311 us so, 316 with two), one where
+    // the rows that four wavefronts share come through registers (2000 rows, 8 heads of 127: 165 us so, 219 with two, which spill).
+    static constexpr int PER_CU = !B16 ? (DP == 64 ? 2 : 1) : LONE ? 1 : DP == 64 && DIRECT && NB == 1 ? 3 : 2;
     static_assert(LDS >= (NB / 2) * NA * DP * 32 * sizeof(float), "room for the sums");
 };
 
@@ -24,9 +30,10 @@ template <typename T, int DP, int NA, int NB, bool DIRECT>
 __global__ __launch_bounds__(ATT_THREADS, (DqShape<T, DP, NA, NB, DIRECT>::PER_CU)) void attention_dq_kernel(AttArgs a)
 {
     typedef Op<T, DP> M;
-    constexpr int BK = DqShape<T, DP, NA, NB, DIRECT>::BK;
+    typedef DqShape<T, DP, NA, NB, DIRECT> Shape;
+    constexpr int BK = Shape::BK;
     extern __shared__ __attribute__((aligned(256))) char lds[];
-    constexpr int TILE = DqShape<T, DP, NA, NB, DIRECT>::TILE;
+    constexpr int TILE = Shape::TILE;
     T *lk = reinterpret_cast<T *>(lds), *lv = lk + TILE;
     AttTile tile;
     const int head = att_head((int)blockIdx.x, a.heads), kvh = head / a.group;
@@ -34,7 +41,9 @@ __global__ __launch_bounds__(ATT_THREADS, (DqShape<T, DP, NA, NB, DIRECT>::PER_C
     const int l = (int)threadIdx.x & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wa = NB == 1 ? w : w % NA, wb = NB == 1 ? 0 : w / NA;
     const int q0 = tile.index * 32 * NA, qw = q0 + wa * 32, qi = qw + (l & 31);
     const bool valid = qi < tile.len;
-    typename M::held q[DP / 16], g[DP / 16];
+    typename M::held q[DP / 16], g[DP / 16 - Shape::HELD];
+    constexpr int HELD = Shape::HELD, REGS = DP / 16 - HELD;
+    typename M::held *held = reinterpret_cast<typename M::held *>(lds + Shape::STAGED) + w * HELD * 64 + l;
     float delta = 0.0f;
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d) {
@@ -48,21 +57,26 @@ __global__ __launch_bounds__(ATT_THREADS, (DqShape<T, DP, NA, NB, DIRECT>::PER_C
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) delta += o.get(j) * go.get(j);
-        g[d] = M::of(go);
+        if (d < REGS) g[d] = M::of(go);
+        else held[64 * (d - REGS)] = M::of(go);
     }
     delta = join_halves<false>(delta);
     const size_t at_row = (size_t)head * a.total + tile.start + qi;
     const float lse_ = valid ? a.lse[at_row] : 0.0f, lse = lse_ * LOG2E;
     load_frags<T, DP>(a.Q, tile.start + qi, head, valid, a.dim, q);
-    // D of the stored O carries O's rounding, which in bf16 is large beside dP - D of rows with few keys.  The sum of a row of dS says by
-    // how much: P sums to one, so that D + sum(dS) is D without it.  The gradients of K and V begin at that; here, it comes too late but
-    // for rows whose keys all lie in the first tile, which pass over it once before.  (Sequences of a few rows: errors against 64 bits
-    // 3.6e-3 -> 2.2e-3, 4 x 2048 rows 2.5e-3 -> 2.4e-3; backward pass of the latter 277 -> 284 us.)
+    // D of the stored O carries O's rounding, which in bf16 is large beside dP - D where the values have a mean (of 64: dQ off by 14 %).
+    // The sum of a row of dS says by how much: P sums to one, so that D + sum(dS) is D without it, at which the gradients of K and V
+    // begin.  Here it is known behind the last key, and dQ = scale (dS K - sum(dS) P K): P K is one product more, with K^T as it is
+    // read for dS K (4 x 2048 rows, 32 heads of 64: 129 -> 148 us).
     constexpr bool CORRECT = sizeof(T) == 2;
     float more = 0.0f;
-    acc16 from = -delta, o[DP / 32];          // dP - D: its sums begin at -D
+    const acc16 from = -delta;                // dP - D: its sums begin at -D
+    acc16 o[DP / 32], pk[CORRECT ? DP / 32 : 1];
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) o[t] = 0.0f;
+    for (int t = 0; t < DP / 32; ++t) {
+        o[t] = 0.0f;
+        if constexpr (CORRECT) pk[t] = 0.0f;
+    }
     const float c = a.scale * LOG2E;
     const int last = min(tile.len, q0 + 32 * NA), nk = (last + BK - 1) / BK;
     AttStage<T, DP, BK, DIRECT> sk, sv;
@@ -113,57 +127,54 @@ __global__ __launch_bounds__(ATT_THREADS, (DqShape<T, DP, NA, NB, DIRECT>::PER_C
             }
         }
         const typename M::Tile tk(lk + 32 * wb * M::PITCH), tv(lv + 32 * wb * M::PITCH);
-        // P (dP - D) of block b, zero where masked
-        auto gradients = [&](int b, acc16 &s) {
+#pragma unroll
+        for (int b = 0; b < BK / 32; b += NB) {
             const int kb = k0 + 32 * (b + wb);
-            acc16 dp = from;
-            s = 0.0f;
+            if (kb > qw + 31) continue;
+            acc16 s = 0.0f, dp = from;
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
                 if (att_empty<T, DP>(d, a.dim)) break;
                 s = M::mma(M::rows(tk, 32 * b, 16 * d), q[d], s);
-                dp = M::mma(M::rows(tv, 32 * b, 16 * d), g[d], dp);
+                dp = M::mma(M::rows(tv, 32 * b, 16 * d), d < REGS ? g[d] : held[64 * (d - REGS)], dp);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse)) * dp[i];
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse));
+                dp[i] *= s[i];
+            }
             if (kb + 31 > qw) {
                 // a row that sees one key has no gradient through the softmax: zero, not the round-off of dP - D
 #pragma unroll
-                for (int i = 0; i < 16; ++i) if (kb + acc_row(i, h) > qi || qi == 0) s[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) {
+                    if (kb + acc_row(i, h) > qi) s[i] = 0.0f;
+                    if (kb + acc_row(i, h) > qi || qi == 0) dp[i] = 0.0f;
+                }
             }
-        };
-        if (CORRECT && kt == 0 && (NB == 1 ? qw + 31 < BK : nk == 1)) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int b = 0; b < BK / 32; b += NB) {
-                if (32 * (b + wb) > qw + 31) continue;
-                acc16 s;
-                gradients(b, s);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum += s[i];
-            }
-            sum = sum_of_row(sum);
-            delta += sum;
-            from = -delta;
-        }
-#pragma unroll
-        for (int b = 0; b < BK / 32; b += NB) {
-            if (k0 + 32 * (b + wb) > qw + 31) continue;
-            acc16 s;
-            gradients(b, s);
             if constexpr (CORRECT) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) more += s[i];
+                for (int i = 0; i < 16; ++i) more += dp[i];
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const typename M::held p = M::pack(s, 8 * k);
+                const typename M::held ds = M::pack(dp, 8 * k);
+                typename M::held p;
+                if constexpr (CORRECT) p = M::pack(s, 8 * k);
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) o[t] = M::mma(M::cols(tk, 32 * b + 16 * k, 32 * t), p, o[t]);
+                for (int t = 0; t < DP / 32; ++t) {
+                    const typename M::frag kc = M::cols(tk, 32 * b + 16 * k, 32 * t);
+                    o[t] = M::mma(kc, ds, o[t]);
+                    if constexpr (CORRECT) pk[t] = M::mma(kc, p, pk[t]);
+                }
             }
         }
     }
-    if constexpr (CORRECT) delta += sum_of_row(more);
+    if constexpr (CORRECT) {
+        const float sum = sum_of_row(more);
+        delta += sum;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) o[t] -= pk[t] * sum;
+    }
     if (valid && h == 0 && wb == 0) {
         a.from[at_row] = -lse_ / a.scale;
         a.from[(size_t)a.heads * a.total + at_row] = -delta;

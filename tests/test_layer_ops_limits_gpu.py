@@ -59,3 +59,63 @@ def test_sequences_of_one_row_have_no_gradient_through_the_softmax(lens, heads, 
     want, size, off = sums(dO.double()), sums(dO.double().abs()), sums(2 * ez[:, :, None] * dO.double().abs())
     assert bool(((dV.double() - want).abs() <= U[dtype] * 1.01 * want.abs() + (2 * 6 * group + 1) * F * size + off).all())
 
+
+# ---- values far from zero mean ----------------------------------------------------------------------
+def _gradients(Q, K, V, dO, cu, scale, heads):
+    """dQ of some heads and dK, dV in 64 bits, and what independent roundings, each of at most half a step, change of dQ and dK in the
+    norm: dS before its sum is taken out (off by P times the rounding of O), P beside it, the results, and fp32 sums of dim products."""
+    group, dim = Q.shape[1] // K.shape[1], Q.shape[2]
+    ref = {"dQ": {}, "dK": torch.zeros(K.shape, dtype=torch.float64, device=DEV), "dV": torch.zeros(V.shape, dtype=torch.float64, device=DEV)}
+    off = {"dQ": {}, "dK": torch.zeros(K.shape, dtype=torch.float64, device=DEV)}         # squares
+    mm = lambda a, b: torch.mm(a.contiguous(), b.contiguous())
+    u = U[bf16] if Q.dtype == bf16 else 0.0
+    for j in range(Q.shape[1]):
+        jk = j // group
+        if j in heads:
+            ref["dQ"][j] = torch.zeros(Q.shape[0], dim, dtype=torch.float64, device=DEV)
+            off["dQ"][j] = torch.zeros(Q.shape[0], dim, dtype=torch.float64, device=DEV)
+        for s, e in zip(cu[:-1], cu[1:]):
+            n = e - s
+            if n == 0:
+                continue
+            q, k, v, g = Q[s:e, j].double(), K[s:e, jk].double(), V[s:e, jk].double(), dO[s:e, j].double()
+            seen = torch.ones(n, n, device=DEV).tril().bool()
+            z = torch.where(seen, scale * mm(q, k.T), -math.inf)
+            P = torch.softmax(z, 1)
+            dP = mm(g, v.T)
+            dS = P * (dP - (P * dP).sum(1, keepdim=True))
+            by_o = (g.abs() * mm(P, v).abs() * U[Q.dtype]).sum(1, keepdim=True)            # of D, by O as stored
+            # P by its exponent and dP, D: sums of dim products, sqrt(dim) F of their size in the mean
+            ez = torch.where(seen, scale * mm(q.abs(), k.abs().T), 0.0).amax(1, keepdim=True) * math.sqrt(dim) * F + 4 * F
+            ed = math.sqrt(dim) * F * (mm(g.abs(), v.abs().T) + (g.abs() * mm(P, v.abs())).sum(1, keepdim=True))
+            each = (u * (dS.abs() + 2 * P * by_o)).square() + (2 * ez * dS.abs() + 2 * P * ed).square()
+            ref["dK"][s:e, jk] += scale * mm(dS.T, q)
+            ref["dV"][s:e, jk] += mm(P.T, g)
+            off["dK"][s:e, jk] += scale ** 2 * mm(each.T, q.square())
+            if j in heads:
+                ref["dQ"][j][s:e] = scale * mm(dS, k)
+                off["dQ"][j][s:e] = scale ** 2 * mm(each, k.square()) + (U[Q.dtype] * ref["dQ"][j][s:e]).square()
+    off["dK"] += (U[Q.dtype] * ref["dK"]).square()
+    return ref, off
+
+
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("lens,heads,kv_heads", [([300], 200, 2), ([129, 0, 700, 65, 1], 2, 1), ([129, 0, 700, 65, 1], 96, 4), ([1500], 40, 8)])
+@pytest.mark.parametrize("dim", [64, 50, 96, 128])
+@pytest.mark.parametrize("mean_v,mean_k", [(1.0, 0.0), (64.0, 0.0), (1.0, 4.0)])
+def test_gradients_do_not_carry_the_rounding_of_o(mean_v, mean_k, dim, lens, heads, kv_heads, dtype):
+    cu, dcu = _offsets(lens)
+    total = cu[-1]
+    Q, dO = _randn(total, heads, dim, dtype=dtype, seed=1), _randn(total, heads, dim, dtype=dtype, seed=4)
+    K, V = _randn(total, kv_heads, dim, dtype=dtype, seed=2, mean=mean_k), _randn(total, kv_heads, dim, dtype=dtype, seed=3, mean=mean_v)
+    _, _, dQ, dK, dV = _train(Q, K, V, dO, dcu)
+    some = sorted({0, heads // 2, heads - 1})
+    ref, off = _gradients(Q, K, V, dO, cu, dim ** -0.5, some)
+    for j in some:
+        for s, e in zip(cu[:-1], cu[1:]):                    # the first tile's rows and the later ones apart
+            for a, b in ((s, min(e, s + 64)), (s + 64, e)):
+                if b > a + 1:
+                    err = float(torch.linalg.norm(dQ[a:b, j].double() - ref["dQ"][j][a:b]))
+                    assert err <= math.sqrt(float(off["dQ"][j][a:b].sum())), (j, a, b, err / float(torch.linalg.norm(ref["dQ"][j][a:b])))
+    assert float(torch.linalg.norm(dK.double() - ref["dK"])) <= math.sqrt(float(off["dK"].sum()))
+    assert float(torch.linalg.norm(dV.double() - ref["dV"]) / torch.linalg.norm(ref["dV"])) <= (math.sqrt(2) * U[bf16] if dtype == bf16 else 1e-5)
