@@ -519,7 +519,8 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  * Sums over a row's keys are divided by the softmax's sum at the end, and may grow to 2^41 times the largest |V|: beyond fp32's
  * range they are infinite.
  * A row depends on no element of another sequence; within a sequence an element of K, V (or of dO, Q in the gradients of K and V) that is
- * no number or infinite may also reach up to 31 rows on the side that the mask hides from it.
+ * no number or infinite may also reach the rows on the side that the mask hides from it within its block of 32 rows, counted from the
+ * sequence's first; in bf16 it may change the roundings of O within its block of 128.
  * The backward pass takes O and lse of the forward pass.  With D_i = dO_i . O_i (bf16: without O's rounding, as the sum of a row of
  * dS gives it), dP = dO V^T, dS = P (dP - D):
  *   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dK and dV summed over the heads that share them,

@@ -127,6 +127,7 @@ __global__ __launch_bounds__(ATT_THREADS, (FwdShape<T, DP, NA, NB, DIRECT>::PER_
             const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
             for (int b = 0; b < NBLK; ++b) {
+                if (b && k0 + 32 * b > qw + 31) continue;    // behind its rows: P is 0, but 0 V is no number where V is infinite
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -from));

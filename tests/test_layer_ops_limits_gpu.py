@@ -119,3 +119,49 @@ def test_gradients_do_not_carry_the_rounding_of_o(mean_v, mean_k, dim, lens, hea
                     assert err <= math.sqrt(float(off["dQ"][j][a:b].sum())), (j, a, b, err / float(torch.linalg.norm(ref["dQ"][j][a:b])))
     assert float(torch.linalg.norm(dK.double() - ref["dK"])) <= math.sqrt(float(off["dK"].sum()))
     assert float(torch.linalg.norm(dV.double() - ref["dV"]) / torch.linalg.norm(ref["dV"])) <= (math.sqrt(2) * U[bf16] if dtype == bf16 else 1e-5)
+
+
+# ---- elements that the mask hides ----------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [bf16, f32])
+@pytest.mark.parametrize("dim", [64, 40, 80, 128, 127])
+@pytest.mark.parametrize("heads", [2, 200])                 # four wavefronts (two) for the same rows; one wavefront for every 32 rows
+@pytest.mark.parametrize("at", [31, 32, 63, 127, 191, 300])
+def test_what_the_mask_hides_reaches_no_row_32_or_more_before_it(at, heads, dim, dtype):
+    n = 340
+    cu, dcu = _offsets([n, 3], lead=5)
+    s, e, r = cu[0], cu[1], cu[0] + at
+    block = s + at // 32 * 32                               # rows before it see nothing of row r's block of 32
+    Q, dO = _randn(cu[-1], heads, dim, dtype=dtype, seed=1), _randn(cu[-1], heads, dim, dtype=dtype, seed=4)
+    K, V = _randn(cu[-1], 1, dim, dtype=dtype, seed=2), _randn(cu[-1], 1, dim, dtype=dtype, seed=3)
+    O, lse, dQ, dK, dV = _train(Q, K, V, dO, dcu)
+    # of an exponent and of a sum of n: twice the dim products of a score, the sum's additions, the logarithm
+    z = dim ** -0.5 * float(torch.linalg.norm(Q.double(), dim=2).max() * torch.linalg.norm(K.double(), dim=2).max())
+    ez = ((2 * dim + 4) * z + n + 8 + 2 * float(lse[:, s:e].abs().max())) * F
+    largest = float(V.abs().max())
+    for bad in (math.inf, -math.inf, math.nan):
+        for t in (K, V):
+            keep = t[r].clone()
+            t[r, 0, dim // 2] = bad
+            o, l, dq = torch.empty_like(O), torch.empty_like(lse), torch.empty_like(dQ)
+            ast.attention(Q, K, V, o, lse=l, cu=dcu)
+            ast.attention_backward(Q, K, V, O, lse, dO, dq, torch.empty_like(dK), torch.empty_like(dV), cu=dcu)
+            t[r] = keep
+            assert torch.equal(dq[s:block], dQ[s:block])
+            # 128 rows share a workgroup, which in bf16 counts its exponents from other maxima where a sum is no number: roundings only
+            tile = block if dtype == f32 else s + at // 128 * 128
+            assert torch.equal(o[s:tile], O[s:tile]) and torch.equal(l[:, s:tile], lse[:, s:tile])
+            off = (o[tile:block].double() - O[tile:block].double()).abs()
+            assert bool((off <= 2 * (2.02 * U[bf16] + 2 * ez) * largest).all())
+            assert bool(((l[:, tile:r] - lse[:, tile:r]).abs() <= 2 * ez).all())
+            if t is V or math.isnan(bad):                   # a score of minus infinity only takes the key away
+                assert not bool(torch.isfinite(o[r]).all())
+            assert torch.equal(o[e:cu[-1]], O[e:cu[-1]]) and torch.equal(dq[e:cu[-1]], dQ[e:cu[-1]])
+        for t in (Q, dO):
+            keep = t[r].clone()
+            t[r, 0, dim // 2] = bad
+            dq, dk, dv = torch.empty_like(dQ), torch.empty_like(dK), torch.empty_like(dV)
+            ast.attention_backward(Q, K, V, O, lse, dO, dq, dk, dv, cu=dcu)
+            t[r] = keep
+            assert torch.equal(dq[s:r], dQ[s:r]) and torch.equal(dq[r + 1:cu[-1]], dQ[r + 1:cu[-1]])
+            for a, b in ((dk, dK), (dv, dV)):
+                assert torch.equal(a[block + 32:cu[-1]], b[block + 32:cu[-1]])
