@@ -165,3 +165,26 @@ def test_what_the_mask_hides_reaches_no_row_32_or_more_before_it(at, heads, dim,
             assert torch.equal(dq[s:r], dQ[s:r]) and torch.equal(dq[r + 1:cu[-1]], dQ[r + 1:cu[-1]])
             for a, b in ((dk, dK), (dv, dV)):
                 assert torch.equal(a[block + 32:cu[-1]], b[block + 32:cu[-1]])
+
+
+# ---- 8-bit output ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("rows,cols,dtype", [(4096, 2048, bf16), (3000, 777, f32), (5000, 100, bf16), (300, 5632, f32)])
+def test_norm_rounds_quotients_to_8_bits(rows, cols, group, dtype):
+    # Y is the nearest 8-bit value, ties to even, of the fp32 quotient of y (a call with fp32 output gives it) and the scale
+    e4m3 = torch.float8_e4m3fn
+    X, R, W = _randn(rows, cols, dtype=dtype, seed=1), _randn(rows, cols, dtype=dtype, seed=2), _randn(cols, seed=3)
+    y, Y = torch.empty(rows, cols, device=DEV), torch.empty(rows, cols, dtype=torch.uint8, device=DEV).view(e4m3)
+    S = torch.empty(rows, -(-cols // 128) if group else 1, device=DEV)
+    W[cols // 2:] *= 1e-32                                  # groups next to the smallest scale
+    X[5], R[5] = X[5] * 2.0 ** -90, 0                       # and a row, with 1 / sqrt(eps) = 1000
+    ast.rms_norm(X, y, W=W, R=R)
+    ast.rms_norm(X, Y, W=W, R=R, scale=S, group=group)
+    spread = S.repeat_interleave(group or cols, 1)[:, :cols]
+    # on the host: the quotient of two fp32 numbers in 64 bits rounds to the same 24 bits, and those to 8 bits by comparison with the
+    # neighbours' middle
+    q = (y.cpu().double() / spread.cpu().double()).float().double()
+    step = torch.exp2(torch.floor(torch.log2(q.abs().clamp_min(2.0 ** -6))) - 3)
+    want = torch.clamp(torch.round(q / step) * step, -448.0, 448.0)
+    assert bool((Y.cpu().float().double() == want).all())
+    assert int((S <= 2.0 ** -80).sum()) >= 1
