@@ -644,7 +644,8 @@ def sym_unpack(items, stream=None) -> None:
 # ---------------------------------------------------------------------------- operators of a decoder layer
 #
 # These calls are short (a few microseconds on the device), so the host's part counts: descriptors are packed in one go, sizes and
-# devices of a tensor read once, and the raw handle of the current stream is taken.
+# devices of a tensor read once, and the raw handle of the current stream is taken (4 us less than the stream object's a call).  A torch
+# without these two has the public ones, and one without a GPU part, where no call gets that far, still imports this.
 
 _RNG = struct.Struct("@QQQf0Q")
 _DROP = struct.Struct("@QQ5i0Q")
@@ -654,7 +655,8 @@ _ATTN = struct.Struct("@6Q8q6if0Q")
 _ATTN_GRAD = struct.Struct("@4Q8q")
 _CODE = {torch.float32: F32, torch.bfloat16: BF16}
 _E4M3 = torch.float8_e4m3fn
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _on(stream, first, *tensors):
