@@ -456,7 +456,8 @@ asteria_status asteria_soap_reproject(const asteria_rblock *blocks, int nblocks,
  *   state             NULL, or device pointer to two uint64 (seed, offset) that are read when the kernel runs, instead of the
  *                     fields: a captured graph that is replayed takes new numbers from there.
  * X: rows x cols, fp32 or bf16; Y of the same type; Y may be X (with ldy = ldx).
- * Errors: NULL X, Y or rng, rows or cols <= 0, ld < cols, bad dtype or p -> INVALID_ARG; more than 2^34 elements -> UNSUPPORTED. */
+ * Errors: NULL X, Y or rng, rows or cols <= 0, ld < cols, bad dtype or p -> INVALID_ARG; rows ceil(cols / 8) > 2^32 - 256 ->
+ * UNSUPPORTED. */
 typedef struct asteria_rng {
     uint64_t seed, offset;
     const uint64_t *state;
@@ -526,7 +527,8 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  *   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO,   dK and dV summed over the heads that share them,
  * without atomics: every run gives the same bits.
  * Errors: NULL pointers, sizes <= 0, heads no multiple of kv_heads, bad dtype, scale not within 2^-100 .. 2^100, negative strides,
- * written arrays that overlap themselves or begin where another array does, cu NULL with nseq > 1 -> INVALID_ARG; dim > 128, or (total / 128 + nseq) heads >= 2^24 -> UNSUPPORTED. */
+ * written arrays that overlap themselves or begin where another array does, cu NULL with nseq > 1 -> INVALID_ARG; dim > 128, or
+ * (floor(total / 128) + 1 + nseq) heads >= 2^24 -> UNSUPPORTED. */
 typedef struct asteria_attn {
     const void *Q, *K, *V;
     void *O; /* written by asteria_attention, read by asteria_attention_backward */
