@@ -188,3 +188,37 @@ def test_norm_rounds_quotients_to_8_bits(rows, cols, group, dtype):
     want = torch.clamp(torch.round(q / step) * step, -448.0, 448.0)
     assert bool((Y.cpu().float().double() == want).all())
     assert int((S <= 2.0 ** -80).sum()) >= 1
+
+
+# ---- fp32's lowest and largest numbers ------------------------------------------------------------------
+@pytest.mark.parametrize("heads", [2, 200])
+@pytest.mark.parametrize("dim", [64, 50, 128])
+@pytest.mark.parametrize("lowest", [torch.finfo(f32).min, -3.397e38, -3.39e38])
+def test_attention_in_fp32_with_numbers_that_round_to_no_bf16(lowest, dim, heads):
+    # keys that are so far down that they count for nothing: results are those of the rows without them
+    n, hidden = 300, [1, 40, 70, 128, 200]
+    Q, K, V, dO = (_randn(n, h, dim, seed=i) for i, h in enumerate((heads, 1, 1, heads)))
+    Q[:, :, 0] = 1.0
+    K[hidden] = 0.0
+    K[hidden, 0, 0] = lowest
+    keep = [i for i in range(n) if i not in hidden]
+    O, lse, dQ, dK, dV = _train(Q, K, V, dO, scale=1.0)
+    q, k, v, z0 = Q.double(), K[keep].double(), V[keep].double(), torch.ones(len(keep), len(keep), device=DEV).tril().bool()
+    for j in (0, heads - 1):
+        z = torch.where(z0, torch.mm(q[keep, j].contiguous(), k[:, 0].T.contiguous()), -math.inf)
+        P = torch.softmax(z, 1)
+        ref = torch.mm(P, v[:, 0].contiguous())
+        # exponents twice, dim products each, and sums of n
+        e = float(torch.where(z0, torch.mm(q[keep, j].abs().contiguous(), k[:, 0].abs().T.contiguous()), 0.0).max()) * (dim + 4) * F
+        tol = (2 * (e + 4 * F) + (2 * n + 10) * F) * torch.mm(P, v[:, 0].abs()) + F * ref.abs()
+        assert bool(((O[keep, j].double() - ref).abs() <= tol).all())
+        want = torch.logsumexp(z, 1)
+        assert bool(((lse[j, keep].double() - want).abs() <= e + (n + 8) * F + 2 * F * want.abs()).all())
+    # the largest and lowest value of one key comes out as it is, in sequences of one row
+    cu = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    big = V.clone()
+    big[:, 0, 0], big[:, 0, 1] = torch.finfo(f32).max, lowest
+    ast.attention(torch.zeros_like(Q), K, big, O, cu=cu)
+    assert torch.equal(O, big.expand(n, heads, dim))
+    # finite gradients, none to keys that count for nothing
+    assert all(bool(torch.isfinite(t).all()) for t in (dQ, dK, dV)) and not bool(dK[hidden].any()) and not bool(dV[hidden].any())
