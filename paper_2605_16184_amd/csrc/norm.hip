@@ -161,8 +161,8 @@ struct NormGradArgs {
 };
 
 // Every workgroup takes rows gridDim.x apart and keeps its columns' share of dW in registers over all of them, so that H and dY are
-// read once and dW costs a row of partial sums a workgroup (600 x 5632: 13.7 us, 2.5 TB/s: three dependent trips to memory and two
-// barriers a row, one or two rows a workgroup).
+// read once and dW costs a row of partial sums a workgroup (600 x 5632: 13.7 us, 2.5 TB/s: two rows a workgroup, of which the second's
+// loads begin behind the first's two barriers).
 template <int TPR, int VPT, typename TH, typename TY>
 __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGradArgs a)
 {

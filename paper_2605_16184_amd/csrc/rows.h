@@ -19,8 +19,6 @@ typedef uint8_t u8x8_any __attribute__((ext_vector_type(8), aligned(1)));
 
 struct bf16_elem { uint16_t bits; };
 
-__device__ __forceinline__ float elem_f32(float v) { return v; }
-__device__ __forceinline__ float elem_f32(bf16_elem v) { return __uint_as_float((uint32_t)v.bits << 16); }
 // to nearest, ties to even; the conversion instruction keeps what is no number
 __device__ __forceinline__ uint16_t f32_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
