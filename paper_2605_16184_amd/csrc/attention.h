@@ -478,7 +478,7 @@ inline int64_t att_tiles(const AttArgs &a, int qt)
 }
 // A wavefront for every 32 rows, four of which share a tile of the rows they pass over - or where that gives less than one and a
 // half workgroups a CU, four wavefronts (or two) for the same 32 rows, each with a quarter (half) of what is passed over.  Forward and backward, heads of
-// 64: at 324 workgroups 101 us so, 104 us otherwise, at 444 155 and 144 us (bf16); 500 and 540, 855 and 757 us (fp32).
+// 64: at 324 workgroups 103 us so, 107 us otherwise, at 444 160 and 150 us (bf16); 304 and 362, 570 and 524 us (fp32).
 inline bool att_few(const AttArgs &a, int heads) { return att_tiles(a, 128) * heads < 384; }
 
 // How many wavefronts the same rows take then.  Tiles of 32 rows for each of them lie in LDS: fp32 ones fill it with two (and a tile that
@@ -488,12 +488,13 @@ template <typename T> constexpr int att_shared = sizeof(T) == 4 ? 2 : 4;
 template <typename T, int DP> __device__ __forceinline__ bool att_empty(int d, int dim) { return sizeof(T) == 4 && DP == 96 && d == 5 && dim <= 80; }
 
 // LDS to ask for, in kernels of which PER_CU workgroups fit a CU.  Workgroups that would all run at once are given so much that fewer
-// share a CU: the longest then do not share one while others stand idle.  fp32, below 1024 workgroups: one (4 x 2048 rows, 8 heads of
-// 64: forward 213 -> 176 us).  bf16, three a CU, below 768: two (backward, heads of 64: 740 workgroups 130 -> 123 us; at 888 146 -> 148).
+// share a CU: the longest then do not share one while others stand idle.  fp32 with two a CU, below 544: one (heads of 64, forward: 390 workgroups
+// 225 -> 218 us, 520 484 -> 476; at 756 200 -> 238).  bf16 with three a CU, below 768: two (backward, heads of 64: 740 workgroups 142 -> 133 us;
+// at 888 159 -> 160).
 template <typename T, int NB, int PER_CU> constexpr size_t att_lds(size_t need, int64_t blocks)
 {
     const size_t more = sizeof(T) == 4 ? 84 * 1024 : 56 * 1024;
-    return NB == 1 && (sizeof(T) == 4 || PER_CU == 3) && blocks < (sizeof(T) == 4 ? 1024 : 768) && need < more ? more : need;
+    return NB == 1 && (sizeof(T) == 4 || PER_CU == 3) && blocks < (sizeof(T) == 4 ? 544 : 768) && need < more ? more : need;
 }
 
 // Kernels for dims padded to 64, 96 or 128.
