@@ -477,8 +477,8 @@ asteria_status asteria_dropout(const asteria_drop *d, const asteria_rng *rng, vo
  * written.  H may be R or X, Y may be X (same type and leading dimension).
  * y_dtype ASTERIA_E4M3: per row (group = 0) or per 128 columns (group = 128, the last group may be shorter)
  * scale = max(largest |y|, 2^-100) / 448 and Y = y / scale rounded to the nearest 8-bit value (ties to even); Scale: fp32, rows x
- * ceil(cols / group), contiguous.  A group with an element that is no number, or infinite, holds no number somewhere; others are
- * not touched by it.
+ * ceil(cols / group), contiguous.  A row with an element that is no number, or infinite, holds no number somewhere in Y; other rows
+ * are not touched by it.  Where the sum of h^2 passes fp32's range (elements around 2^63) the row of Y is zero.
  * The backward pass takes the sum H as stored: with r = 1 / sqrt(mean(h^2) + eps), n = dY w,
  *   dR = dH + r (n - h r^2 mean(n h)),   dX = drop(dR),   dW = sum over rows of dY h r,
  * dH: the gradient that reaches H by the residual path, or NULL.  dX, dR, dW: NULL = not written.  dR may be dH, dX may be dY
@@ -514,11 +514,14 @@ asteria_status asteria_rms_norm_backward(const asteria_norm_grad *n, float eps, 
  * int32[nseq + 1], ascending, within 0 .. total (read when the kernel runs; numbers outside are brought inside, but a descending
  * cu gives unspecified results); NULL: one sequence of `total` rows, nseq = 1.
  * Element (i, j, d) of Q lies at Q + i ldq + j hq + d, likewise the others: any strides and alignment; of written arrays rows
- * and heads may not overlap, nor one another or an array that is read.  dtype fp32 or bf16; products on the bf16 matrix cores with fp32 sums, softmax in fp32.  bf16: P (and dS
- * in the backward pass) is rounded to bf16 as an operand of the next product.  fp32: every operand is cut into three bf16 terms,
- * which keeps it to 2^-27; an infinite element has no such terms and counts as no number.  dim 1 .. 128.
- * Sums over a row's keys are divided by the softmax's sum at the end, and may grow to 2^41 times the largest |V|: beyond fp32's
- * range they are infinite.
+ * and heads may not overlap, nor one another or an array that is read.  dtype fp32 or bf16; products on the bf16 matrix cores with
+ * fp32 sums, softmax in fp32.  bf16: P (and dS in the backward pass) is rounded to bf16 as an operand of the next product.  fp32: every
+ * operand is cut into three bf16 terms, which keeps it to 2^-27, or to 2^-134 where that is more; an infinite element has no such terms and
+ * counts as no number.  dim 1 .. 128.
+ * Scores count in powers of two: z log2(e) beyond fp32's range is infinite.  Sums over a row's keys are divided by the softmax's sum at the
+ * end, and may grow to 2^41 times the largest |V|: beyond fp32's range they are infinite.
+ * How the rows are dealt to workgroups goes by total and nseq, not by what cu holds: sequences of no rows at the end of a cu of fixed
+ * length cost a workgroup a head each that finds nothing to do, and with more than 64 entries tiles go in order, not longest first.
  * A row depends on no element of another sequence; within a sequence an element of K, V (or of dO, Q in the gradients of K and V) that is
  * no number or infinite may also reach the rows on the side that the mask hides from it within its block of 32 rows, counted from the
  * sequence's first; in bf16 it may change the roundings of O within its block of 128.

@@ -222,3 +222,29 @@ def test_attention_in_fp32_with_numbers_that_round_to_no_bf16(lowest, dim, heads
     assert torch.equal(O, big.expand(n, heads, dim))
     # finite gradients, none to keys that count for nothing
     assert all(bool(torch.isfinite(t).all()) for t in (dQ, dK, dV)) and not bool(dK[hidden].any()) and not bool(dV[hidden].any())
+
+
+@pytest.mark.parametrize("exponent", [-100, -115, -126, -133])
+@pytest.mark.parametrize("dtype", [bf16, f32])
+def test_attention_with_the_smallest_numbers(exponent, dtype):
+    # sequences of one row give V back: fp32 as three bf16 terms, of which the last ends at bf16's smallest step, 2^-133
+    n = 64
+    V = ((1 + torch.rand(n, 2, 64, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)) * 2.0 ** exponent).to(dtype)
+    Z, O = torch.zeros_like(V), torch.empty_like(V)
+    ast.attention(Z, Z, V, O, cu=torch.arange(n + 1, dtype=torch.int32, device=DEV))
+    assert float((O.double() - V.double()).abs().max()) <= (0.0 if dtype == bf16 else 2.0 ** -134)
+
+
+def test_norm_of_rows_that_hold_no_number_or_pass_the_range():
+    X = _randn(8, 300, seed=1)
+    clean, S0 = torch.empty(8, 300, device=DEV).to(torch.float8_e4m3fn), torch.empty(8, 3, device=DEV)
+    ast.rms_norm(X, clean, scale=S0, group=128)
+    X[1, 5], X[3, 299], X[5] = math.nan, -math.inf, 1e20
+    Y, S, Z = torch.empty_like(clean), torch.empty_like(S0), torch.empty(8, 300, device=DEV)
+    ast.rms_norm(X, Y, scale=S, group=128)
+    ast.rms_norm(X, Z)
+    same = [0, 2, 4, 6, 7]
+    assert torch.equal(Y[same].view(torch.uint8), clean[same].view(torch.uint8)) and torch.equal(S[same], S0[same])
+    for r in (1, 3):
+        assert not bool(torch.isfinite(Y[r].float()).all()) and not bool(torch.isfinite(Z[r]).all())
+    assert not bool(Y[5].float().any()) and not bool(Z[5].any())
