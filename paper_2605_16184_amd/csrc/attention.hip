@@ -18,10 +18,9 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct FwdShape {
 // by tile through two stages of LDS: the next tile is on its way while this one is multiplied, with one barrier a tile.
 // Bound by the vector units more than by the matrix cores: 32 x 32 scores and their products with a head of 64 are 256 cycles of the
 // latter, their exponentials, sums and roundings 1.5 times as many of the former, and up to four wavefronts a SIMD overlap them.
-// Measured: 8192 rows, 32 heads of 64 on 4 (275 GFLOP of causal products): 282 - 290 us, 950 - 975 TFLOP/s, matrix cores busy 50 % and
-// vector units 72 % of the time at 1.8 - 1.95 GHz (the power limit), no LDS conflicts; 4 x 2048 rows 85 us, 8123 packed rows, 16 heads
-// of 128: 81 us.
-// fp32: 4 x 2048 rows, 16 heads of 64: 209 us.
+// Measured, calls back to back: 8192 rows, 32 heads of 64 on 4 (275 GFLOP of causal products): 287 - 292 us, 940 - 960 TFLOP/s, matrix cores
+// busy 49 % and vector units 70 % of the time at 1.8 - 1.95 GHz (the power limit), no LDS conflicts; 4 x 2048 rows 85 - 91 us, 8123 packed
+// rows, 16 heads of 128: 81 us.  fp32: 4 x 2048 rows, 16 heads of 64: 209 - 215 us.
 template <typename T, int DP, int NA, int NB, bool DIRECT>
 __global__ __launch_bounds__(ATT_THREADS, (FwdShape<T, DP, NA, NB, DIRECT>::PER_CU)) void attention_kernel(AttArgs a)
 {

@@ -1,10 +1,11 @@
 // Gradients of K and V (attention.h): a wavefront holds the keys and values of 32 rows in registers and passes over the
 // rows that see them, in all the heads that share them.
 //
-// Four products a tile; accumulators and the held keys and values leave room for three wavefronts a SIMD (heads of up to 64; two with
-// longer ones), of which 1.8 (1.6) are resident on average, and that bounds it: matrix cores and vector units are busy 35 % of the time.
-// Measured: 4 x 2048 rows, 32 heads of 64 on 4: 145 us, 940 TFLOP/s of causal products; 8123 packed rows, 16 heads of 128 on 4: 157 us.
-// With 64 keys a wavefront the backward pass of the former took 365 instead of 325 us.
+// Four products a tile; accumulators and the held keys and values leave room for three wavefronts a SIMD (heads of up to 64; two
+// with longer ones), of which 2.3 (1.6) are resident on average, and that bounds it: matrix cores are busy 43 % (37 %) and vector units 43 % (28 %)
+// of the time.  Three registers of a lane (one) lie in scratch memory over the loop.
+// Measured: 4 x 2048 rows, 32 heads of 64 on 4: 149 us, 920 TFLOP/s of causal products; 8123 packed rows, 16 heads of 128 on 4: 158 us.
+// With 64 keys a wavefront the backward pass of the former took 12 % more.
 //
 // Where the heads that share keys are many and the tiles are few, several workgroups take a part of these heads each, leave
 // their sums in fp32 in the workspace, and a second kernel adds them up: without atomics, in one order.
@@ -24,7 +25,7 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> struct DkvShape {
     static constexpr int HELD = WIDE ? 3 : 0;
     static constexpr size_t SUMS = (NB / 2) * NA * DP * 32 * sizeof(float), STAGED = (DIRECT ? 2 : 1) * (2 * TILE * sizeof(T) + 2 * ROWS * sizeof(float)) + HELD * NA * 64 * 16;
     static constexpr size_t LDS = STAGED > SUMS ? STAGED : SUMS;
-    // Workgroups a CU.  Three with heads of up to 64 in bf16: the backward pass of 4 x 2048 rows, 32 heads, 302 us with two, 284 us so.
+    // Workgroups a CU.  Three with heads of up to 64 in bf16: the backward pass of 4 x 2048 rows, 32 heads, 326 us with two, 306 us so.
     static constexpr int PER_CU = sizeof(T) == 4 ? 1 : DP == 64 && DIRECT ? 3 : DP == 64 || DIRECT ? 2 : 1;
 };
 
@@ -219,7 +220,7 @@ template <typename T, int DP, int NA, int NB, bool DIRECT> hipError_t launch(con
 }  // namespace
 
 // The sums of a part of the heads are written and read once more in fp32, so as few parts as give the card four workgroups a CU:
-// the backward pass of 4 x 2048 rows, 32 heads on 4, 284 us, 302 with 1536 and 343 with 512 workgroups as the mark.
+// the backward pass of 4 x 2048 rows, 32 heads on 4, 306 us, 323 with 1536 and 372 with 512 workgroups as the mark.
 int asteria::attention_splits(const AttArgs &a)
 {
     const int64_t tiles = att_tiles(a, 128) * (a.heads / a.group);

@@ -2,8 +2,8 @@
 //
 // The tiles and stages of the forward pass, with three products a tile instead of two (four in bf16).  A kernel of its own, beside that
 // of K and V, which computes scores and dP once more: one kernel for all would add dQ up over workgroups, by atomics whose order
-// changes the result or through partial sums in memory (570 MB for 4 x 2048 rows, 32 heads of 64).  Measured: those rows 148 us, 930
-// TFLOP/s of causal products; 8123 packed rows, 16 heads of 128: 148 us.
+// changes the result or through partial sums in memory (570 MB for 4 x 2048 rows, 32 heads of 64).  Measured: those rows 147 us, 940
+// TFLOP/s of causal products, matrix cores busy 41 % and vector units 47 %, 2.2 wavefronts a SIMD; 8123 packed rows, 16 heads of 128: 146 us.
 #include "attention.h"
 #include "gemm.h"
 
@@ -13,15 +13,15 @@ namespace {
 
 template <typename T, int DP, int NA, int NB, bool DIRECT> struct DqShape {
     static constexpr bool B16 = sizeof(T) == 2, LONE = B16 && NB > 1 && !DIRECT && DP > 64;
-    // 32 keys a stage where registers are short: two blocks side by side take 16 more of them.  4 x 2048 rows, 16 heads of 128, backward:
-    // 322 us so, 353 with 64 keys; heads of 65 in rows of no whole pieces: 497 and 507 us.
+    // 32 keys a stage where registers are short: two blocks side by side take 16 more of them.  8123 packed rows, 16 heads of 128, backward:
+    // 316 us so, 399 with 64 keys; 4 x 2048 rows, 16 heads of 65 in rows of no whole pieces: 497 and 528 us.
     static constexpr int BK = 32 * (NB > 1 ? NB : B16 && (DP == 128 || (DP == 96 && !DIRECT)) ? 1 : Op<T, DP>::BLOCKS);
     static constexpr int TILE = BK * Op<T, DP>::PITCH;
     // Pieces of dO that stay in LDS, so that two accumulators of dim x 32 fit the registers of PER_CU workgroups.
     static constexpr int HELD = !B16 || LONE ? 0 : DP == 64 ? (DIRECT && NB == 1 ? 2 : 0) : DP == 96 ? 3 : DIRECT ? 5 : 7;
     static constexpr size_t STAGED = (DIRECT ? 4 : 2) * (size_t)TILE * sizeof(T), LDS = STAGED + HELD * NA * NB * 64 * 16;
-    // Workgroups a CU: three with heads of up to 64 in bf16 (backward pass of 4 x 2048 rows, 32 heads: 311 us so, 316 with two), one where
-    // the rows that four wavefronts share come through registers (2000 rows, 8 heads of 127: 165 us so, 219 with two, which spill).
+    // Workgroups a CU: three with heads of up to 64 in bf16 (backward pass of 4 x 2048 rows, 32 heads: 306 us so, 319 with two), one where
+    // the rows that four wavefronts share come through registers (2000 rows, 8 heads of 127, backward: 166 us so, 225 with two, which spill).
     static constexpr int PER_CU = !B16 ? (DP == 64 ? 2 : 1) : LONE ? 1 : DP == 64 && DIRECT && NB == 1 ? 3 : 2;
     static_assert(LDS >= (NB / 2) * NA * DP * 32 * sizeof(float), "room for the sums");
 };
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(ATT_THREADS, (DqShape<T, DP, NA, NB, DIRECT>::PER_C
     // D of the stored O carries O's rounding, which in bf16 is large beside dP - D where the values have a mean (of 64: dQ off by 14 %).
     // The sum of a row of dS says by how much: P sums to one, so that D + sum(dS) is D without it, at which the gradients of K and V
     // begin.  Here it is known behind the last key, and dQ = scale (dS K - sum(dS) P K): P K is one product more, with K^T as it is
-    // read for dS K (4 x 2048 rows, 32 heads of 64: 129 -> 148 us).
+    // read for dS K (4 x 2048 rows, 32 heads of 64: 129 -> 147 us).
     constexpr bool CORRECT = sizeof(T) == 2;
     float more = 0.0f;
     const acc16 from = -delta;                // dP - D: its sums begin at -D

@@ -3,7 +3,7 @@
 // A row lies in the registers of TPR threads, VPT chunks of eight elements each, chunk v * TPR + thread: every array is read
 // and written once, in 16-byte (bf16) or 32-byte (fp32) pieces per thread, and what bounds both passes is memory.  Sums over
 // a row (fp32) go over 16 lanes (rows of up to 128 elements), over the lanes of one wavefront (up to 2048) or through LDS.
-// Measured: 16384 x 2048, bf16 with residual, sum, dropout and 8-bit output (236 MB) 49.6 us, 4.8 TB/s, the rate of a large copy;
+// Measured: 16384 x 2048, bf16 with residual, sum, dropout and 8-bit output (236 MB) 50.8 us, 4.6 TB/s, a large copy's rate being 4.9;
 // 1001 x 777 in fp32 5.1 us; 4 rows of 2048 4.1 us, launch and the latency of one row.  Backward, 16384 x 2048 with fp32 residual
 // stream (537 MB): 114 us, 4.7 TB/s, both kernels.
 #include <math.h>
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_kernel(NormArgs a)
         const float scale = fmaxf(top[v], SCALE_FLOOR) / E4M3_MAX, inv = 1.0f / scale;
         if (a.group ? (ch & 15) == 0 : ch == 0) a.Scale[(size_t)row * groups + (a.group ? ch >> 4 : 0)] = scale;
         // Quotients: a product with the rounded reciprocal is on the other side of a tie for some elements.  The product's remainder, exact in one
-        // multiply-add, times the reciprocal once more rounds it to the quotient (16384 x 2048: 52 us, 57 with divisions) - but not
+        // multiply-add, times the reciprocal once more rounds it to the quotient (16384 x 2048: 53.7 us, 57 with divisions, where a product took 53) - but not
         // where the remainder can pass below fp32's range or the scale is infinite.  |y / scale| is at most 448 (1 + 2^-22), which rounds to
         // 448; what is no number stays none
         float z[8];
@@ -161,7 +161,7 @@ struct NormGradArgs {
 };
 
 // Every workgroup takes rows gridDim.x apart and keeps its columns' share of dW in registers over all of them, so that H and dY are
-// read once and dW costs a row of partial sums a workgroup (600 x 5632: 13.7 us, 2.5 TB/s: two rows a workgroup, of which the second's
+// read once and dW costs a row of partial sums a workgroup (600 x 5632: 13.4 us, 2.6 TB/s: two rows a workgroup, of which the second's
 // loads begin behind the first's two barriers).
 template <int TPR, int VPT, typename TH, typename TY>
 __global__ __launch_bounds__(norm_threads<TPR>()) void norm_grad_kernel(NormGradArgs a)
