@@ -126,7 +126,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_kernel(NormArgs a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float near = h[v][e] * inv;
-                z[e] = __builtin_fmaf(__builtin_fmaf(-near, scale, h[v][e]), inv, near);
+                z[e] = __builtin_fmaf(-__builtin_fmaf(near, scale, -h[v][e]), inv, near);     // in this order -0 stays -0
             }
         } else {
 #pragma unroll

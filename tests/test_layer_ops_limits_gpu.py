@@ -235,6 +235,18 @@ def test_attention_with_the_smallest_numbers(exponent, dtype):
     assert float((O.double() - V.double()).abs().max()) <= (0.0 if dtype == bf16 else 2.0 ** -134)
 
 
+@pytest.mark.parametrize("group", [0, 128])
+def test_norm_in_8_bits_keeps_the_sign_of_zero(group):
+    X, W = _randn(40, 300, seed=1), _randn(300, seed=2)
+    X[:, ::3] = 0.0
+    X[:, 1::7] = 0.0                                        # times weights of both signs
+    y, Y = torch.empty_like(X), torch.empty(40, 300, dtype=torch.uint8, device=DEV)
+    S = torch.empty(40, 3 if group else 1, device=DEV)
+    ast.rms_norm(X, y, W=W)
+    ast.rms_norm(X, Y.view(torch.float8_e4m3fn), W=W, scale=S, group=group)
+    assert torch.equal(Y >= 128, torch.signbit(y)) and bool((torch.signbit(y) & (y == 0)).any())
+
+
 def test_norm_of_rows_that_hold_no_number_or_pass_the_range():
     X = _randn(8, 300, seed=1)
     clean, S0 = torch.empty(8, 300, device=DEV).to(torch.float8_e4m3fn), torch.empty(8, 3, device=DEV)
